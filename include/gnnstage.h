@@ -368,6 +368,31 @@ int gnnstage_profile_read(gnnstage_t *st, int32_t kind, int32_t layer, double *m
 int gnnstage_profile_reset(gnnstage_t *st);
 
 /*
+ * Rows kept in 8 bits (activation checkpoints): what a forward pass saves for the weight gradients takes 33/64 of its bf16 size.
+ * Blocks of 32 columns share a power of two: with a the block's largest magnitude, e is the least whole number in [-120, 121]
+ * with a <= 127 * 2^e, every value is kept as q = x / 2^e rounded to the nearest whole number (ties to even, within [-127, 127]),
+ * and stands for q * 2^e, exactly a bf16 and an fp32 number.  A value is off by at most half of 2^e (blocks above 127 * 2^121: by 2^e).
+ * scale holds the byte e + 127; 255: the block had an infinity or a NaN, all of it restores to NaN.
+ * q: DEVICE, 16-byte aligned, rows x ld_q bytes, ld_q a multiple of 16 and at least d rounded up to 32 (zeros from d on); scale:
+ * DEVICE, rows x ld_s, ld_s >= (d + 31) / 32.  x, dY: DEVICE, of dtype (GNNSTAGE_F32 / GNNSTAGE_BF16), leading dimensions of any size from the width on.
+ *   gnnstage_rows8_store        q, scale from x (rows x d)
+ *   gnnstage_rows8_load         x from q, scale
+ *   gnnstage_rows8_weight_grad  dW (fp32 d x d_out) += X^T dY, dbias (fp32 d_out, may be NULL) += column sums of dY, with X the stored rows:
+ *                               products of exactly the stored values, fp32 sums in a fixed order.  workspace: DEVICE, 256-byte aligned, of
+ *                               gnnstage_rows8_weight_grad_workspace_size() bytes, nothing to be cleared or kept; calls that overlap in time need
+ *                               workspaces of their own.
+ * They only launch kernels on hip_stream.  Message of an error: gnnstage_last_error(NULL).
+ */
+int gnnstage_rows8_store(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t d, int8_t *q, int64_t ld_q, uint8_t *scale,
+                         int64_t ld_s, void *hip_stream);
+int gnnstage_rows8_load(const int8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, int64_t rows, int32_t d, void *x,
+                        int32_t dtype, int64_t ld_x, void *hip_stream);
+size_t gnnstage_rows8_weight_grad_workspace_size(int64_t rows, int32_t d, int32_t d_out, int32_t dtype);
+int gnnstage_rows8_weight_grad(const int8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, const void *dY, int32_t dtype,
+                               int64_t ld_dy, int64_t rows, int32_t d, int32_t d_out, float *dW, float *dbias, void *workspace,
+                               size_t workspace_bytes, void *hip_stream);
+
+/*
  * Diagnostic: what this GPU's memory system gives the access pattern of the aggregation (Algorithm 1's AGGREGATE
  * line reads one embedding row per neighbour), with no arithmetic and no index traffic around it.  Every 16-lane
  * group reads whole rows of row_bytes (a multiple of 256, at most 4096) at pseudo-random row numbers, eight rows in

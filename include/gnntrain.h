@@ -110,6 +110,24 @@ int gnntrain_softmax_xent(const float *logits, int32_t ld, const float *bias, co
                           const uint8_t *mask, int64_t rows, int32_t n_classes, float inv_n_train, void *dlogits,
                           int32_t dl_dtype, int32_t dl_ld, float *row_loss, void *hip_stream);
 
+/* The loss head over many classes: what a linear classifier, gnntrain_softmax_xent and the classifier's gradients compute, without
+ * the logits of all rows and classes in memory at any time.  z = h_r W + bias; for a labelled row: row_loss = log sum_c
+ * exp(z_c) - z_label, g_c = (softmax_c - [c = label]) * inv_n_train; dh = g W^T, dW += h^T g, db += column sums of g.  A row is
+ * labelled when mask (NULL: all rows) is non-zero and its label is in [0, n_classes); any other row has loss 0 and a zero row of
+ * dh, takes no part in dW and db whatever it holds, and may hold anything.
+ * h: DEVICE rows x d, leading dimension ld_h >= d; W: DEVICE d x n_classes, both of dtype; bias: DEVICE fp32 n_classes or NULL
+ * (minus infinity leaves a class out; a row whose every logit is minus infinity has loss and gradients NaN).  labels, mask, row_loss: DEVICE, by row.
+ * dh (of dtype, leading dimension ld_dh), dW (fp32 d x n_classes), db (fp32 n_classes): DEVICE, each may be NULL; all NULL: the losses
+ * alone.  Outputs may not overlap inputs.  bf16 products have fp32 sums; the factors of dW are held to 16 bits.  Sums are added in a fixed order: the same call gives
+ * the same bits.
+ * workspace: DEVICE, 256-byte aligned, of gnntrain_head_xent_workspace_size(); written by the call, nothing in it has to be
+ * cleared or kept.  Calls that overlap in time need workspaces of their own, and so do graphs that are replayed side by side.
+ * The call only launches kernels (asynchronous, may be captured).  Message of an error: gnntrain_last_error(NULL). */
+size_t gnntrain_head_xent_workspace_size(int64_t rows, int32_t d, int32_t n_classes, int32_t dtype, int32_t want_grads);
+int gnntrain_head_xent(const void *h, int64_t ld_h, const void *W, int32_t dtype, const float *bias, const int32_t *labels,
+                       const uint8_t *mask, int64_t rows, int32_t d, int32_t n_classes, float inv_n_train, float *row_loss, void *dh,
+                       int64_t ld_dh, float *dW, float *db, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* out[0] = scale * sum of x[0 .. n), added in a fixed order (reproducible).  scratch: DEVICE, 1024 floats. */
 int gnntrain_sum(const float *x, int64_t n, float scale, float *scratch, float *out, void *hip_stream);
 

@@ -174,6 +174,24 @@ def _load():
     lib.gnntrain_sgd_step.restype = C.c_int
     lib.gnntrain_sgd_step.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_float,
                                       C.c_void_p]
+    lib.gnntrain_head_xent_workspace_size.restype = C.c_size_t
+    lib.gnntrain_head_xent_workspace_size.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+    lib.gnntrain_head_xent.restype = C.c_int
+    lib.gnntrain_head_xent.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32,
+                                       C.c_int32, C.c_float, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_size_t, C.c_void_p]
+    # rows kept in 8 bits
+    lib.gnnstage_rows8_store.restype = C.c_int
+    lib.gnnstage_rows8_store.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p,
+                                         C.c_int64, C.c_void_p]
+    lib.gnnstage_rows8_load.restype = C.c_int
+    lib.gnnstage_rows8_load.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int32,
+                                        C.c_int64, C.c_void_p]
+    lib.gnnstage_rows8_weight_grad_workspace_size.restype = C.c_size_t
+    lib.gnnstage_rows8_weight_grad_workspace_size.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32]
+    lib.gnnstage_rows8_weight_grad.restype = C.c_int
+    lib.gnnstage_rows8_weight_grad.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_int64,
+                                               C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     return lib
 
 
@@ -337,6 +355,147 @@ def _ptrs(tensors: Sequence) -> "C.Array":
     for i, t in enumerate(tensors):
         arr[i] = None if t is None else t.data_ptr()
     return arr
+
+
+# ---- operators on tensors ------------------------------------------------------------------
+def _refuse(name: str, why: str):
+    raise GnnStageError(-1, f"{name}: {why}")
+
+
+def _dtype_code(name: str, what: str, t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return GNNSTAGE_BF16
+    if t.dtype != torch.float32:
+        _refuse(name, f"{what} must be float32 or bfloat16, not {t.dtype}")
+    return GNNSTAGE_F32
+
+
+def _tensor(name: str, what: str, t, shape, dtype, device) -> None:
+    """A tensor on the call's device, of this type and shape, with its elements side by side."""
+    if t.device != device:
+        _refuse(name, f"{what} is on {t.device}, not on {device}")
+    if t.dtype != dtype:
+        _refuse(name, f"{what} must be {dtype}, not {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        _refuse(name, f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if not t.is_contiguous():
+        _refuse(name, f"{what} must be contiguous")
+
+
+def _matrix(name: str, what: str, t, shape, dtype, device) -> int:
+    """The same for a matrix whose rows may be further apart than they are wide; its leading dimension."""
+    if t.device != device:
+        _refuse(name, f"{what} is on {t.device}, not on {device}")
+    if t.dtype != dtype:
+        _refuse(name, f"{what} must be {dtype}, not {t.dtype}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        _refuse(name, f"{what} must have the shape {'rows x columns' if shape is None else tuple(shape)}, not {tuple(t.shape)}")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        _refuse(name, f"the columns of {what} must be side by side")
+    if rows <= 1:
+        return max(cols, t.stride(0))
+    if t.stride(0) < cols:
+        _refuse(name, f"the rows of {what} overlap")
+    return t.stride(0)
+
+
+def _room(name: str, workspace, device):
+    import torch
+    if workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        _refuse(name, f"workspace must be a contiguous uint8 tensor on {device}")
+    return workspace.data_ptr(), workspace.numel()
+
+
+class _On:
+    """The call's device is the current one inside, and its current stream is the call's."""
+
+    def __init__(self, name: str, device):
+        import torch
+        if device.type != "cuda":
+            _refuse(name, f"tensors must be on a GPU, not on {device}")
+        self._guard = torch.cuda.device(device)
+        self._device = device
+
+    def __enter__(self):
+        import torch
+        self._guard.__enter__()
+        return C.c_void_p(torch.cuda.current_stream(self._device).cuda_stream)
+
+    def __exit__(self, *exc):
+        return self._guard.__exit__(*exc)
+
+
+def _stored(name: str, q, scale, device):
+    import torch
+    ld_q = _matrix(name, "q", q, None, torch.int8, device)
+    ld_s = _matrix(name, "scale", scale, None, torch.uint8, device)
+    if scale.shape[0] != q.shape[0] or q.shape[1] != 32 * scale.shape[1]:
+        _refuse(name, f"q of {tuple(q.shape)} needs a scale of {(q.shape[0], q.shape[1] // 32)}, not {tuple(scale.shape)}: a byte per 32 columns")
+    return (ld_q + 15) // 16 * 16 if q.shape[0] <= 1 else ld_q, ld_s
+
+
+def gnnstage_rows8_store(x, q, scale) -> None:
+    """Keeps the rows of ``x`` (fp32 or bf16, rows x d) in 8 bits: ``q`` int8 [rows, d rounded up to 32], ``scale`` uint8
+    [rows, q's columns / 32]."""
+    name = "gnnstage_rows8_store"
+    dt = _dtype_code(name, "x", x)
+    ld_x = _matrix(name, "x", x, None, x.dtype, x.device)
+    ld_q, ld_s = _stored(name, q, scale, x.device)
+    rows, d = x.shape
+    if tuple(q.shape) != (rows, (d + 31) // 32 * 32):
+        _refuse(name, f"q must have the shape {(rows, (d + 31) // 32 * 32)}, not {tuple(q.shape)}")
+    with _On(name, x.device) as stream:
+        rc = lib.gnnstage_rows8_store(x.data_ptr(), dt, ld_x, rows, d, q.data_ptr(), ld_q, scale.data_ptr(), ld_s, stream)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
+
+
+def gnnstage_rows8_load(q, scale, x) -> None:
+    """Restores rows into ``x`` (fp32 or bf16, rows x d)."""
+    name = "gnnstage_rows8_load"
+    dt = _dtype_code(name, "x", x)
+    ld_x = _matrix(name, "x", x, None, x.dtype, x.device)
+    ld_q, ld_s = _stored(name, q, scale, x.device)
+    rows, d = x.shape
+    if tuple(q.shape) != (rows, (d + 31) // 32 * 32):
+        _refuse(name, f"q must have the shape {(rows, (d + 31) // 32 * 32)}, not {tuple(q.shape)}")
+    with _On(name, x.device) as stream:
+        rc = lib.gnnstage_rows8_load(q.data_ptr(), ld_q, scale.data_ptr(), ld_s, rows, d, x.data_ptr(), dt, ld_x, stream)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
+
+
+def gnnstage_rows8_weight_grad_workspace_size(rows: int, d: int, d_out: int, dtype: int) -> int:
+    size = int(lib.gnnstage_rows8_weight_grad_workspace_size(int(rows), int(d), int(d_out), int(dtype)))
+    if size == 0:
+        raise GnnStageError(-1, lib.gnnstage_last_error(None).decode())
+    return size
+
+
+def gnnstage_rows8_weight_grad(q, scale, dY, dW, workspace, dbias=None) -> None:
+    """``dW`` (fp32 [d, d_out]) += stored rows^T ``dY``, ``dbias`` (fp32 [d_out]) += column sums of ``dY`` (fp32 or bf16)."""
+    import torch
+    name = "gnnstage_rows8_weight_grad"
+    dt = _dtype_code(name, "dY", dY)
+    dev = dY.device
+    ld_q, ld_s = _stored(name, q, scale, dev)
+    if dW.dim() != 2 or dY.dim() != 2:
+        _refuse(name, "dW and dY must be matrices")
+    d, d_out = dW.shape
+    if q.shape[1] != (d + 31) // 32 * 32:
+        _refuse(name, f"q has {q.shape[1]} columns, dW has {d} rows")
+    ld_dy = _matrix(name, "dY", dY, (q.shape[0], d_out), dY.dtype, dev)
+    _tensor(name, "dW", dW, (d, d_out), torch.float32, dev)
+    if dbias is not None:
+        _tensor(name, "dbias", dbias, (d_out,), torch.float32, dev)
+    ws, size = _room(name, workspace, dev)
+    with _On(name, dev) as stream:
+        rc = lib.gnnstage_rows8_weight_grad(q.data_ptr(), ld_q, scale.data_ptr(), ld_s, dY.data_ptr(), dt, ld_dy, q.shape[0], d, d_out,
+                                            dW.data_ptr(), None if dbias is None else dbias.data_ptr(), ws, size, stream)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
 
 
 class GnnStage:
@@ -554,6 +713,43 @@ def gnntrain_softmax_xent(logits, bias, labels, mask, n_classes: int, inv_n_trai
         dlogits.stride(0) if rows else max(n_classes, 1), row_loss.data_ptr(), _cur_stream())
     if rc != 0:
         raise GnnStageError(rc, "gnntrain_softmax_xent")
+
+
+def gnntrain_head_xent_workspace_size(rows: int, d: int, n_classes: int, dtype: int, want_grads: bool = True) -> int:
+    size = int(lib.gnntrain_head_xent_workspace_size(int(rows), int(d), int(n_classes), int(dtype), int(bool(want_grads))))
+    if size == 0:
+        raise GnnStageError(-1, lib.gnntrain_last_error(None).decode())
+    return size
+
+
+def gnntrain_head_xent(h, W, bias, labels, mask, inv_n_train: float, row_loss, workspace, dh=None, dW=None, db=None) -> None:
+    """Row losses of the linear softmax cross-entropy head and, where given, its gradients, without the logits in memory.  h: fp32 or bf16
+    [rows, d]; W: same type [d, n_classes]; bias fp32 [n_classes] or None; labels int32 [rows]; mask uint8 [rows] or None; row_loss fp32
+    [rows]; dh: h's type [rows, d]; dW fp32 [d, n_classes] and db fp32 [n_classes] are added to."""
+    import torch
+    name = "gnntrain_head_xent"
+    dt = _dtype_code(name, "h", h)
+    dev = h.device
+    ld_h = _matrix(name, "h", h, None, h.dtype, dev)
+    rows, d = h.shape
+    if W.dim() != 2:
+        _refuse(name, "W must be a matrix")
+    n_classes = W.shape[1]
+    _tensor(name, "W", W, (d, n_classes), h.dtype, dev)
+    _tensor(name, "labels", labels, (rows,), torch.int32, dev)
+    _tensor(name, "row_loss", row_loss, (rows,), torch.float32, dev)
+    for what, t, shape, dtype in (("bias", bias, (n_classes,), torch.float32), ("mask", mask, (rows,), torch.uint8),
+                                  ("dW", dW, (d, n_classes), torch.float32), ("db", db, (n_classes,), torch.float32)):
+        if t is not None:
+            _tensor(name, what, t, shape, dtype, dev)
+    ld_dh = d if dh is None else _matrix(name, "dh", dh, (rows, d), h.dtype, dev)
+    ws, size = _room(name, workspace, dev)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    with _On(name, dev) as stream:
+        rc = lib.gnntrain_head_xent(h.data_ptr(), ld_h, W.data_ptr(), dt, ptr(bias), labels.data_ptr(), ptr(mask), rows, d, n_classes,
+                                    float(inv_n_train), row_loss.data_ptr(), ptr(dh), ld_dh, ptr(dW), ptr(db), ws, size, stream)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnntrain_last_error(None).decode())
 
 
 def gnntrain_sum(x, scale: float, scratch, out) -> None:

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <string>
+
 typedef __bf16 bf16_t;
 
 // Which chunks count as processed (Section 3.3, V_processed), one bit per chunk id.
@@ -307,7 +309,7 @@ int launch_spmm_dense(const DenseArgs &a, hipStream_t s);
 int launch_dense_expand(const int64_t *blk_e0, const uint16_t *ent_pos, const uint32_t *ent_w, void *tiles, int64_t n_blocks,
                         hipStream_t s);
 
-enum DType : int { DT_F32 = 0, DT_BF16 = 1 };
+enum DType : int { DT_F32 = 0, DT_BF16 = 1, DT_ROWS8 = 2 };  // DT_ROWS8: kept in 8 bits, see rows8.hip
 
 // src dtype -> out dtype; returns hipError_t as int.  launch_spmm runs the per-task kernel,
 // launch_spmm_reduce adds the pieces of long rows (needed whenever a.n_long > 0).
@@ -380,6 +382,9 @@ struct GemmTnArgs {
   int32_t max_splits;
   float *dbias;         // optional: dbias[o] += column sums of B, fused into the product
   float *bias_partial;  // fp32 scratch [splits][O]
+  const uint8_t *a_scale = nullptr;  // a_dtype DT_ROWS8: the factors of A's rows, a byte per 32 columns
+  int32_t ld_scale = 0;
+  int32_t b_cols = 0;             // columns of B that may be read (0: ldb)
   int32_t wide_min_rows = 65536;  // bf16 operands from this many rows on, with more than one 128 x 128 output tile: one
                                   // workgroup per row split computes the whole output (tests force it on small inputs)
 };
@@ -436,6 +441,12 @@ int launch_ln_param_reduce(const LnReduceArgs *red, int n, hipStream_t s);
 // dst[r][c] = src[r][c] for c < d, zero for d <= c < dst_ld
 int launch_copy_rows(const void *src, int src_ld, void *dst, int dst_ld, int64_t M, int d, int dtype, hipStream_t s);
 
+// ---- rows in 8 bits -----------------------------------------------------------------------------
+// q (16-byte aligned, ld_q a multiple of 16 and at least d rounded up to 32, written up to there) and scale (a byte per 32 columns) from
+// rows of any alignment
+int launch_rows8_store(const void *x, int dtype, int64_t ld, int64_t rows, int d, int8_t *q, int64_t ld_q, uint8_t *scale, int64_t ld_s,
+                       hipStream_t s);
+
 // ---- small kernels ------------------------------------------------------------------------
 // Wt[N][Kp] (transposed) and Wn[K][Np] (plain) zero-padded copies of W[K][N] in the compute dtype
 struct StageWeightsArgs {
@@ -470,5 +481,9 @@ constexpr int kFills = 32;
 // symmetric normalisation weights from row lengths: val[e] = 1/sqrt(len(row) * len(other))
 int launch_gcn_norm(const int64_t *ptr, const uint32_t *pidx, int vbits, const int64_t *len_ptr, int64_t n,
                     float *val, hipStream_t s);
+
+// The last error of entry points without a handle: what gnntrain_last_error(NULL) and gnnstage_last_error(NULL) tell.  Return code.
+int train_error(int code, const std::string &msg);
+int stage_error(int code, const std::string &msg);
 
 static inline int round_up(int x, int m) { return (x + m - 1) / m * m; }

@@ -11,6 +11,7 @@
 // it is read element-wise with bounds checks and converted while it is staged into LDS.
 #include <algorithm>
 #include <functional>
+#include <type_traits>
 
 #include "common.h"
 
@@ -198,6 +199,18 @@ __device__ inline bf16x8 load8_bf16(const T *base, size_t ld, int r, int c, int 
 #pragma unroll
     for (int t = 0; t < 8; ++t)
       if (c + t < cols) out[t] = (bf16_t)to_f32(p[t]);
+  }
+  return out;
+}
+
+// 8 consecutive columns (from a multiple of 8 on) of a row kept in 8 bits, exactly as bf16; columns >= cols read as zero
+__device__ inline bf16x8 load8_rows8(const int8_t *q, size_t ld, const uint8_t *scale, size_t ld_scale, int r, int c, int cols) {
+  bf16x8 out = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (c < cols) {
+    const u32x2 w = *reinterpret_cast<const u32x2 *>(q + (size_t)r * ld + c);
+    const float f = __builtin_bit_cast(float, (uint32_t)scale[(size_t)r * ld_scale + (c >> 5)] << 23);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) out[t] = (bf16_t)((float)(int8_t)(w[t >> 2] >> (8 * (t & 3))) * f);
   }
   return out;
 }
@@ -670,7 +683,8 @@ __global__ __launch_bounds__(256) void gemm_tn_bf16_kernel(const Batch<GemmTnWor
   const TA *A = static_cast<const TA *>(a.A);
   const bf16_t *B = static_cast<const bf16_t *>(a.B);
   const bf16x8 zero8 = {0, 0, 0, 0, 0, 0, 0, 0};
-  const int a_cols = VEC ? a.lda : a.I;
+  constexpr bool ROWS8 = std::is_same<TA, int8_t>::value;
+  const int a_cols = ROWS8 ? (a.I + 31) / 32 * 32 : VEC ? a.lda : a.I;
 
   f32x16 acc[2][2];
 #pragma unroll
@@ -713,8 +727,11 @@ __global__ __launch_bounds__(256) void gemm_tn_bf16_kernel(const Batch<GemmTnWor
     for (int i = 0; i < NVT; ++i) {
       const int r = 2 * ((tid >> 4) + 16 * (i >> 1)) + (i & 1), c = (tid & 15) * 8;  // slots 2h, 2h+1: one row pair
       const bool rv = r0 + r < r_end;
-      if constexpr (!PAIR) ra[i] = rv ? load8_bf16<TA, VEC>(A, (size_t)a.lda, r0 + r, i0 + c, a_cols) : zero8;
-      rb[i] = (rv && o0 + c < a.ldb) ? *reinterpret_cast<const bf16x8 *>(B + (size_t)(r0 + r) * a.ldb + o0 + c) : zero8;
+      if constexpr (ROWS8)
+        ra[i] = rv ? load8_rows8(A, (size_t)a.lda, a.a_scale, (size_t)a.ld_scale, r0 + r, i0 + c, a_cols) : zero8;
+      else if constexpr (!PAIR)
+        ra[i] = rv ? load8_bf16<TA, VEC>(A, (size_t)a.lda, r0 + r, i0 + c, a_cols) : zero8;
+      rb[i] = (rv && o0 + c < a.b_cols) ? *reinterpret_cast<const bf16x8 *>(B + (size_t)(r0 + r) * a.ldb + o0 + c) : zero8;
     }
   };
   if (r_begin < r_end) gload(r_begin);
@@ -792,6 +809,8 @@ __global__ __launch_bounds__(256) void gemm_tn_bf16_kernel(const Batch<GemmTnWor
 // only in part through their XCD's L2 (measured on 10 M rows: 16.1 GB fetched for 10.2 GB of operands).  A wave owns
 // 64 rows x 128 columns of the output (eight 32 x 32 accumulators); both operands are bf16 with 16-byte aligned rows.
 constexpr int LDS_PW = 260;  // padded stride, in words, of one row pair of a 256-column LDS tile
+// TA: bf16_t, or int8_t for A rows kept in 8 bits
+template <typename TA>
 __global__ __launch_bounds__(512) void gemm_tn_bf16_wide_kernel(const Batch<GemmTnWork> ba) {
   const GemmTnWork &work_of = ba.sub[blockIdx.z];
   const GemmTnArgs a = work_of.a;
@@ -804,7 +823,7 @@ __global__ __launch_bounds__(512) void gemm_tn_bf16_wide_kernel(const Batch<Gemm
   const int wi = (wave >> 1) * 64, wo = (wave & 1) * 128;
   const int r_begin = split * rows_per_split;
   const int r_end = min(a.M, r_begin + rows_per_split);
-  const bf16_t *A = static_cast<const bf16_t *>(a.A);
+  const TA *A = static_cast<const TA *>(a.A);
   const bf16_t *B = static_cast<const bf16_t *>(a.B);
   const bf16x8 zero8 = {0, 0, 0, 0, 0, 0, 0, 0};
 
@@ -830,8 +849,11 @@ __global__ __launch_bounds__(512) void gemm_tn_bf16_wide_kernel(const Batch<Gemm
     for (int i = 0; i < NVT; ++i) {
       const int r = 2 * ((tid >> 5) + 16 * (i >> 1)) + (i & 1);  // slots 2h, 2h+1: one row pair
       const bool rv = r0 + r < r_end;
-      ra[i] = (rv && c < a.lda) ? *reinterpret_cast<const bf16x8 *>(A + (size_t)(r0 + r) * a.lda + c) : zero8;
-      rb[i] = (rv && c < a.ldb) ? *reinterpret_cast<const bf16x8 *>(B + (size_t)(r0 + r) * a.ldb + c) : zero8;
+      if constexpr (std::is_same<TA, int8_t>::value)
+        ra[i] = rv ? load8_rows8(A, (size_t)a.lda, a.a_scale, (size_t)a.ld_scale, r0 + r, c, (a.I + 31) / 32 * 32) : zero8;
+      else
+        ra[i] = (rv && c < a.lda) ? *reinterpret_cast<const bf16x8 *>(A + (size_t)(r0 + r) * a.lda + c) : zero8;
+      rb[i] = (rv && c < a.b_cols) ? *reinterpret_cast<const bf16x8 *>(B + (size_t)(r0 + r) * a.ldb + c) : zero8;
     }
   };
   if (r_begin < r_end) gload(r_begin);
@@ -1142,7 +1164,9 @@ __global__ __launch_bounds__(256) void gemm_nt_f32_kernel(const GemmNtArgs a) {
 // 10.4 GFLOP over 5,196 rows (1000 x 1000): 160 -> 112 us (93 TFLOP/s); 34 k rows,
 // 100 x 100 outputs: 24 -> 18 us; the bias gradient (column sums of B) rides along, 17 - 27 us as a kernel of its own
 // before.
-template <int V>
+// ROWS8: A rows are kept in 8 bits.  Their rows are zero from I up to a multiple of 32, so that the last vector of one stays where it is
+// (moved back it could have columns of two blocks, and the start of no word).
+template <int V, bool ROWS8 = false>
 __global__ __launch_bounds__(256) void gemm_tn_f32_kernel(const Batch<GemmTnWork> ba) {
   const GemmTnWork &work_of = ba.sub[blockIdx.z];
   const GemmTnArgs a = work_of.a;
@@ -1163,8 +1187,11 @@ __global__ __launch_bounds__(256) void gemm_tn_f32_kernel(const Batch<GemmTnWork
   const int r_begin = split * rows_per_split;
   const int r_end = min(a.M, r_begin + rows_per_split);
   const int lr = lane >> 4, lc = (lane & 15) * V;
-  const int ci = min(i0 + lc, a.I - V), co = min(o0 + lc, a.O - V);
+  static_assert(!ROWS8 || V == 4 || V == 1, "a word or a byte per lane");
+  const int ci = ROWS8 ? min(i0 + lc, (a.I + 31) / 32 * 32 - V) : min(i0 + lc, a.I - V), co = min(o0 + lc, a.O - V);
   const float *A = static_cast<const float *>(a.A) + ci;
+  const int8_t *A8 = static_cast<const int8_t *>(a.A) + ci;
+  const uint8_t *S8 = a.a_scale + (ci >> 5);
   const float *B = static_cast<const float *>(a.B) + co;
   f32x4 acc[V][V], sum[V][V];
 #pragma unroll
@@ -1181,7 +1208,20 @@ __global__ __launch_bounds__(256) void gemm_tn_f32_kernel(const Batch<GemmTnWork
   auto load = [&](int i, int u) {
     const int r = r_begin + (wave + 4 * i) * 4 + lr;
     const size_t rr = (size_t)(r < r_end ? r : r_end - 1);
-    const vec_t x = *reinterpret_cast<const vec_t *>(A + rr * a.lda), y = *reinterpret_cast<const vec_t *>(B + rr * a.ldb);
+    const vec_t y = *reinterpret_cast<const vec_t *>(B + rr * a.ldb);
+    vec_t x;
+    if constexpr (ROWS8) {
+      const float f = __builtin_bit_cast(float, (uint32_t)S8[rr * a.ld_scale] << 23);
+      uint32_t w;
+      if constexpr (V == 4)
+        w = *reinterpret_cast<const uint32_t *>(A8 + rr * a.lda);
+      else
+        w = (uint32_t)(uint8_t)A8[rr * a.lda];
+#pragma unroll
+      for (int t = 0; t < V; ++t) x[t] = (float)(int8_t)(w >> (8 * t)) * f;
+    } else {
+      x = *reinterpret_cast<const vec_t *>(A + rr * a.lda);
+    }
 #pragma unroll
     for (int t = 0; t < V; ++t) {
       fa[u][t] = x[t];
@@ -1261,8 +1301,8 @@ __global__ __launch_bounds__(256) void gemm_tn_f32_kernel(const Batch<GemmTnWork
   float *P = a.partial + (size_t)split * a.I * a.O;
   for (int idx = tid; idx < T * T; idx += 256) {
     const int r = idx / T, c = idx % T, rv = i0 + r / V * V, cv = o0 + c / V * V;  // first columns of the two vectors
-    if (rv < a.I && cv < a.O)
-      P[(size_t)(min(rv, a.I - V) + r % V) * a.O + min(cv, a.O - V) + c % V] = (red[0][idx] + red[1][idx]) + (red[2][idx] + red[3][idx]);
+    if ((ROWS8 ? i0 + r < a.I : rv < a.I) && cv < a.O)
+      P[(size_t)(ROWS8 ? i0 + r : min(rv, a.I - V) + r % V) * a.O + min(cv, a.O - V) + c % V] = (red[0][idx] + red[1][idx]) + (red[2][idx] + red[3][idx]);
   }
   if (do_bias && tid < T && o0 + tid / V * V < a.O)
     a.bias_partial[(size_t)split * a.O + min(o0 + tid / V * V, a.O - V) + tid % V] = (bred[0][tid] + bred[1][tid]) + (bred[2][tid] + bred[3][tid]);
@@ -1463,8 +1503,11 @@ struct TnPlan {
   unsigned gx, threads;
   size_t count() const { return (size_t)w.a.I * w.a.O; }
 };
-static int plan_gemm_tn(const GemmTnArgs &a, int compute_dtype, TnPlan &p) {
-  const bool narrow = a.I < 4 || a.O < 4;  // fp32 operands of fewer columns than a 16-byte vector
+static int plan_gemm_tn(const GemmTnArgs &a_in, int compute_dtype, TnPlan &p) {
+  GemmTnArgs a = a_in;
+  const bool rows8 = a.a_dtype == DT_ROWS8;
+  if (a.b_cols == 0) a.b_cols = a.ldb;
+  const bool narrow = (a.I < 4 && !rows8) || a.O < 4;  // fp32 operands of fewer columns than a 16-byte vector
   const int tile = compute_dtype == DT_BF16 ? 128 : narrow ? 16 : 64;
   const int step = compute_dtype == DT_BF16 ? TR : 16;
   const int ti = (a.I + tile - 1) / tile, to = (a.O + tile - 1) / tile;
@@ -1481,8 +1524,8 @@ static int plan_gemm_tn(const GemmTnArgs &a, int compute_dtype, TnPlan &p) {
   if (splits < 1) splits = 1;
   if (splits > a.max_splits) splits = a.max_splits;
   // long operands with more than one 128 x 128 output tile: one workgroup per row split computes all of the output
-  const bool wide = compute_dtype == DT_BF16 && a.a_dtype == DT_BF16 && a.M >= a.wide_min_rows && ti * to > 1 && a.I <= 256 &&
-                    a.O <= 256 && vec_ok(a.A, a.lda, 8) && vec_ok(a.B, a.ldb, 8);
+  const bool wide = compute_dtype == DT_BF16 && (a.a_dtype == DT_BF16 || rows8) && a.M >= a.wide_min_rows && ti * to > 1 && a.I <= 256 &&
+                    a.O <= 256 && (rows8 || vec_ok(a.A, a.lda, 8)) && vec_ok(a.B, a.ldb, 8);
   if (wide) splits = a.max_splits < 256 ? a.max_splits : 256;  // one workgroup per compute unit
   int rows_per = (a.M + splits - 1) / splits;
   rows_per = (rows_per + step - 1) / step * step;
@@ -1490,16 +1533,19 @@ static int plan_gemm_tn(const GemmTnArgs &a, int compute_dtype, TnPlan &p) {
   p.w = GemmTnWork{a, rows_per, splits};
   p.threads = wide ? 512 : 256;
   if (wide) {
-    p.fn = gemm_tn_bf16_wide_kernel;
+    p.fn = rows8 ? gemm_tn_bf16_wide_kernel<int8_t> : gemm_tn_bf16_wide_kernel<bf16_t>;
     p.gx = (unsigned)splits;
   } else if (compute_dtype == DT_BF16) {
     p.gx = (unsigned)(((splits + 7) / 8) * 8 * ti * to);
-    p.fn = a.a_dtype == DT_F32 ? (pair_ok(a.A, a.lda) ? gemm_tn_bf16_kernel<float, false, true> : gemm_tn_bf16_kernel<float, false>)
+    p.fn = rows8 ? gemm_tn_bf16_kernel<int8_t, true> : a.a_dtype == DT_F32 ? (pair_ok(a.A, a.lda) ? gemm_tn_bf16_kernel<float, false, true> : gemm_tn_bf16_kernel<float, false>)
                                : (vec_ok(a.A, a.lda, 8) ? gemm_tn_bf16_kernel<bf16_t, true> : gemm_tn_bf16_kernel<bf16_t, false>);
   } else {
-    if (a.a_dtype != DT_F32) return hipErrorInvalidValue;
+    if (a.a_dtype != DT_F32 && !rows8) return hipErrorInvalidValue;
     p.gx = (unsigned)((splits * ti * to + 7) / 8 * 8);
-    p.fn = narrow ? gemm_tn_f32_kernel<1> : gemm_tn_f32_kernel<4>;
+    if (rows8)
+      p.fn = narrow ? gemm_tn_f32_kernel<1, true> : gemm_tn_f32_kernel<4, true>;
+    else
+      p.fn = narrow ? gemm_tn_f32_kernel<1> : gemm_tn_f32_kernel<4>;
   }
   return hipSuccess;
 }

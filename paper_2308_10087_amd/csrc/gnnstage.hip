@@ -1665,6 +1665,11 @@ extern "C" int64_t gnnstage_dense_entries(const gnnstage_t *st, int32_t transpos
   return st->dense_entries[transposed ? 1 : 0];
 }
 
+int stage_error(int code, const std::string &msg) {
+  g_create_error = msg;
+  return code;
+}
+
 extern "C" const char *gnnstage_last_error(const gnnstage_t *st) { return st ? st->err.c_str() : g_create_error.c_str(); }
 
 namespace {

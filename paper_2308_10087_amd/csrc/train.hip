@@ -314,6 +314,11 @@ int launch_sum(const float *x, int64_t n, float scale, float *scratch, float *ou
 
 }  // namespace
 
+int train_error(int code, const std::string &msg) {
+  g_create_error = msg;
+  return code;
+}
+
 extern "C" int gnntrain_chunk_order(uint64_t seed, int64_t epoch, int32_t n_chunks, int32_t shuffle, int32_t *order) try {
   if (!order || n_chunks <= 0 || epoch < 0) return GNNSTAGE_EINVAL;
   for (int i = 0; i < n_chunks; ++i) order[i] = i;
