@@ -329,6 +329,832 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
   return hipSuccess;
 }
 
+// ---- bf16 rows of up to 256 columns: the logits never leave the registers -----------------------------------------------------
+// Two kernels of one shape.  A wave OWNS 32 vectors (rows, or classes) whose products' sums it keeps, and the other side is
+// STREAMED past it in tiles of 32 vectors:
+//
+//   rows kernel     owns rows, streams classes:  z[c][i] = W_c . h_i;  p = exp(z - running max);  sum_c p W_c, sum_c p
+//   classes kernel  owns classes, streams rows:  z[i][c] = h_i . W_c;  g = exp(z - log l_i) (label: -o_i / l_i);  sum_i g h_i, sum_i g
+//
+// The first product's result has the streamed index in its registers and the owned one in its lanes (32 x 32 x 16 matrix
+// instructions: register i of lane l is streamed vector 8 (i / 4) + 4 (l / 32) + i % 4, owned vector l % 32), which is the layout of
+// the second product's right operand if its reduction index runs in the order 8 (j / 4) + 4 (l / 32) + j % 4: p goes from one
+// product to the next without leaving its lane.  The left operand of the second product is the streamed tile turned by the LDS
+// transpose reads, four rows of one column per lane at a time, in that same order.  So one LDS copy of a tile, loaded by the
+// direct-to-LDS path, serves both products.
+// Bound by the matrix cores: per owned and streamed vector 4 d operations (rows kernel), 6 d (classes kernel: g enters as the sum
+// of two bf16 numbers, since dW is fp32), per wave and tile 32 (48) matrix instructions at d = 256 and half the LDS bandwidth.
+// Two workgroups of four waves per compute unit: one's exponentials run under the other's products.
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef bf16_t bf16x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+#define LDS_AS __attribute__((address_space(3)))
+typedef LDS_AS char lds_char;
+
+constexpr float kLog2e = 1.44269504088896f;
+constexpr float kNoMax = -3.4028234663852886e38f;  // the least number: of a row that has seen no more than minus infinity
+// exp(z - m): the difference first, so that it is exact for the logits that count, however large they are
+__device__ __forceinline__ float exp_diff(float z, float m) { return __builtin_amdgcn_exp2f((z - m) * kLog2e); }
+constexpr int kTile = 32;           // streamed vectors of a step
+constexpr int kOwned = 128;         // owned vectors of a workgroup, 32 per wave
+constexpr int kRound = 512;         // workgroups that run at once, two per compute unit
+constexpr int kRowItems = 1536;     // most (row tile, class range) pairs that leave partial sums
+constexpr int kMetaBlock = 2048;    // rows of a counting workgroup
+
+// What depends on the number of labelled rows, which the host does not know.
+struct Meta {
+  int32_t n;               // labelled rows
+  int32_t row_tiles;       // of kOwned
+  int32_t splits;          // class ranges of the rows kernel
+  int32_t tiles_per;       // class tiles of a range
+  int32_t rows_per;        // rows of a row range of the classes kernel (a multiple of kTile)
+  int32_t ranges;          // row ranges
+  int32_t unused[2];
+};
+
+// 16-byte pieces of an LDS tile row are permuted by the row, so that neither the row-wise reads of the first product (32 rows, one
+// column piece) nor the transpose reads of the second (four rows, 64 bytes) meet in a bank: no conflicts counted at width 256.
+template <int DP>
+__host__ __device__ constexpr int swizzle(int row) {
+  return DP >= 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
+template <int DP>
+struct Geometry {
+  static constexpr int row_bytes = DP * 2, chunks = DP / 8, rows_per_load = 64 / chunks, loads = kTile / (4 * rows_per_load);
+  static constexpr int tile_bytes = kTile * row_bytes;
+};
+__device__ __forceinline__ void load_lds16(const void *g, lds_char *l) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g, (LDS_AS void *)l, 16, 0, 0);
+}
+// A lane's places in a tile: of what it loads, of its rows in the first product, of its columns in the second.
+template <int DP>
+struct Places {
+  uint32_t load, first, second;
+  __device__ Places(int wave, int lane) {
+    typedef Geometry<DP> G;
+    const int row = wave * G::rows_per_load + lane / G::chunks;
+    load = row * G::row_bytes + (((lane % G::chunks) ^ swizzle<DP>(row)) << 4);
+    const int r = lane & 31, h = lane >> 5;
+    first = r * G::row_bytes + ((h ^ swizzle<DP>(r)) << 4);
+    const int in_half = (lane >> 4) & 1, t = (lane & 15) >> 2, u = lane & 3;  // transpose read: row t, 4 columns from 16 in_half + 4 u
+    second = (4 * h + t) * G::row_bytes + (((2 * in_half + (u >> 1)) ^ swizzle<DP>(4 * h + t)) << 4) + (u & 1) * 8;
+  }
+  // the addresses below are these with constant bits turned over; made anew in every step, or the compiler keeps them all in
+  // registers and spills
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(first), "+v"(second)); }
+};
+template <int DP>
+__device__ __forceinline__ void load_tile(const bf16_t *src, lds_char *dst, int wave, uint32_t place) {
+  typedef Geometry<DP> G;
+#pragma unroll
+  for (int q = 0; q < G::loads; ++q) {
+    constexpr int step = 4 * G::rows_per_load;
+    // (the q-th load's row is step rows on: its swizzle differs where step / 4 is odd)
+    const uint32_t turn = (swizzle<DP>(q * step) ^ swizzle<DP>(0)) << 4;
+    load_lds16(reinterpret_cast<const char *>(src) + (place ^ turn) + q * step * G::row_bytes, dst + q * step * G::row_bytes + wave * 1024);
+  }
+}
+template <int DP>
+__device__ __forceinline__ bf16x8 first_operand(const lds_char *tile, uint32_t place, int ks) {
+  return *reinterpret_cast<const LDS_AS bf16x8 *>(tile + (place ^ ((32 * ks) & (Geometry<DP>::row_bytes - 1) & 255)) + ((32 * ks) & ~255));
+}
+template <int DP>
+__device__ __forceinline__ bf16x8 second_operand(const lds_char *tile, uint32_t place, int dt, int t) {
+  typedef Geometry<DP> G;
+  const uint32_t at = (place ^ ((dt & 3) * 64)) + (dt >> 2) * 256 + 16 * t * G::row_bytes;
+  // (the second half is 8 rows on: swizzle turned over in its second bit)
+  const uint32_t at2 = (place ^ ((dt & 3) * 64 + 32)) + (dt >> 2) * 256 + (16 * t + 8) * G::row_bytes;
+  const bf16x4 x = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + at)));
+  const bf16x4 y = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + at2)));
+  return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// The owned vectors as right operands of the first product: most in registers; the rest, where the registers do not reach, in LDS.
+template <int DP, int IN_REGS>
+struct Owned {
+  static constexpr int steps = DP / 16, in_lds = steps - IN_REGS;
+  bf16x8 reg[IN_REGS];
+  lds_char *lds;
+  __device__ __forceinline__ Owned(const bf16_t *vectors, int64_t first, int wave, int lane, char *shared) {
+    lds = (lds_char *)shared + wave * in_lds * 1024 + lane * 16;
+    const bf16_t *v = vectors + (size_t)(first + (lane & 31)) * DP + 8 * (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < steps; ++i) {
+      const bf16x8 x = *reinterpret_cast<const bf16x8 *>(v + 16 * i);
+      if (i < IN_REGS)
+        reg[i] = x;
+      else
+        *reinterpret_cast<LDS_AS bf16x8 *>(lds + (i - IN_REGS) * 1024) = x;  // read by this lane alone
+    }
+  }
+  __device__ __forceinline__ bf16x8 operator()(int ks) const {
+    return ks < IN_REGS ? reg[ks < IN_REGS ? ks : 0] : *reinterpret_cast<const LDS_AS bf16x8 *>(lds + (ks - IN_REGS) * 1024);
+  }
+};
+template <int DP>
+__device__ __forceinline__ void clear(f32x16 (&o)[DP / 32]) {
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+    for (int t = 0; t < 16; ++t) o[i][t] = 0.f;
+}
+__device__ __forceinline__ void wait_tile() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // this wave's loads to LDS are there (vmcnt 0) ...
+  __syncthreads();                     // ... and everybody's; what the other buffer held is done with
+}
+
+struct RowsArgs {
+  const Meta *meta;
+  const bf16_t *rows, *W;   // packed [.][DP]
+  const float *bias;        // padded to whole tiles with minus infinity
+  const int32_t *label;     // packed
+  const int32_t *list;      // packed row -> row
+  int32_t C, d;
+  float inv_n;
+  float *row_loss;          // by row
+  bf16_t *dh;               // by row, or NULL
+  int64_t ld_dh;
+  float *max, *log, *t;     // packed: the row's maximum, -log2 of its sum, o / l
+  float *part;              // [item][wave][DP][32]: sum p W
+  float *part_stat;         // [item][3][kOwned]: maximum, others, the label's logit
+};
+
+// The end of a row, from its maximum, the others' sum and the label's logit.
+struct RowEnd {
+  float inv, t, loss, log;
+};
+__device__ inline RowEnd end_row(float m, float others, float zl) {
+  const float y = zl - m, own = exp_diff(zl, m), sum = others + own;
+  RowEnd e;
+  e.inv = 1.f / sum;
+  e.t = others / sum;
+  e.loss = own > 0.5f * sum ? log1pf(others / own) : logf(sum) - y;
+  e.log = -log2f(sum);  // (apart from the maximum, which may be so large that a sum of the two has lost it)
+  return e;
+}
+
+template <int DP, bool GRAD, int IN_REGS>
+__global__ __launch_bounds__(256, 2) void head_rows_kernel(const RowsArgs a) {
+  typedef Geometry<DP> G;
+  typedef Owned<DP, IN_REGS> Own;
+  __shared__ __attribute__((aligned(1024))) char tile0[G::tile_bytes];
+  __shared__ __attribute__((aligned(1024))) char tile1[G::tile_bytes];
+  __shared__ __attribute__((aligned(16))) float bias0[kTile];
+  __shared__ __attribute__((aligned(16))) float bias1[kTile];
+  __shared__ __attribute__((aligned(16))) char shared[Own::in_lds > 0 ? 4 * Own::in_lds * 1024 : 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const Meta &meta = *a.meta;
+  const int splits = meta.splits, item = blockIdx.x, row_tile = item / splits, split = item - row_tile * splits;
+  if (row_tile >= meta.row_tiles) return;
+  const int first = row_tile * kOwned + wave * 32;
+  const Own own(a.rows, first, wave, lane, shared);
+  const int label = a.label[first + (lane & 31)];
+  f32x16 sum[DP / 32];
+  clear<DP>(sum);
+  float m = kNoMax, others = 0.f, zl = -INFINITY;
+  Places<DP> at(wave, lane);
+  const int tiles = (a.C + kTile - 1) / kTile, begin = split * meta.tiles_per, end = min(tiles, begin + meta.tiles_per);
+  auto load = [&](int tile, lds_char *dst, float *bias) {
+    load_tile<DP>(a.W + (size_t)tile * kTile * DP, dst, wave, at.load);
+    if (threadIdx.x < kTile / 4) load_lds16(a.bias + (size_t)tile * kTile + threadIdx.x * 4, (lds_char *)bias);
+  };
+  auto step = [&](int tile, const lds_char *now, const float *bias, lds_char *next, float *next_bias) {
+    wait_tile();
+    if (tile + 1 < end) load(tile + 1, next, next_bias);
+    at.renew();
+    f32x16 z;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + 8 * q + 4 * h);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[4 * q + r] = b[r];
+    }
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(first_operand<DP>(now, at.first, ks), own(ks), z, 0, 0, 0);
+    float most = z[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) most = fmaxf(most, z[i]);
+    // The maximum follows only where a logit is more than 5 above it: p then stays below e^5, and the sums are rarely rescaled.
+    if (__any(most > m + 5.f)) {
+      const float up = fmaxf(m, fmaxf(most, __shfl_xor(most, 32))), f = exp_diff(m, up);
+      m = up;
+      others *= f;
+      if constexpr (GRAD) {
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+          for (int t = 0; t < 16; ++t) sum[i][t] *= f;
+      }
+    }
+    const int rel = label - tile * kTile;
+    if (__any((uint32_t)rel < (uint32_t)kTile)) {  // the label's own term is kept out of the sums
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (rel == 8 * (i >> 2) + 4 * h + (i & 3)) {
+          zl = z[i];
+          z[i] = -INFINITY;
+        }
+    }
+    bf16x8 p[2];
+    float part = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float x = exp_diff(z[i], m);
+      part += x;
+      p[i >> 3][i & 7] = (bf16_t)x;  // dh is bf16: the rounding of a factor is no more than its own
+    }
+    others += part;
+    if constexpr (GRAD) {
+#pragma unroll
+      for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(second_operand<DP>(now, at.second, dt, t), p[t], sum[dt], 0, 0, 0);
+    }
+  };
+  if (begin < end) load(begin, (lds_char *)tile0, bias0);
+  for (int tile = begin; tile < end; tile += 2) {
+    step(tile, (const lds_char *)tile0, bias0, (lds_char *)tile1, bias1);
+    if (tile + 1 < end) step(tile + 1, (const lds_char *)tile1, bias1, (lds_char *)tile0, bias0);
+  }
+  others += __shfl_xor(others, 32);
+  zl = __shfl(zl, (lane & 31) + 32 * ((label >> 2) & 1));  // from the half that had the label
+  const int i = first + (lane & 31);
+  if (splits > 1) {
+    float *stat = a.part_stat + (size_t)item * 3 * kOwned + wave * 32 + (lane & 31);
+    if (h == 0) {
+      stat[0] = m;
+      stat[kOwned] = others;
+      stat[2 * kOwned] = zl;
+    }
+    if constexpr (GRAD) {
+      float *out = a.part + ((size_t)item * 4 + wave) * DP * 32 + (lane & 31);
+#pragma unroll
+      for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int t = 0; t < 16; ++t) out[(32 * dt + 8 * (t >> 2) + 4 * h + (t & 3)) * 32] = sum[dt][t];
+    }
+    return;
+  }
+  if (i >= meta.n) return;
+  const RowEnd e = end_row(m, others, zl);
+  const int64_t row = a.list[i];
+  if (h == 0) {
+    a.row_loss[row] = e.loss;
+    a.max[i] = m;
+    a.log[i] = e.log;
+    a.t[i] = e.t;
+  }
+  if constexpr (GRAD) {
+    if (a.dh == nullptr) return;
+    const bf16_t *wy = a.W + (size_t)label * DP;
+    bf16_t *dh = a.dh + (size_t)(row * a.ld_dh);
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = 32 * dt + 8 * q + 4 * h;
+        const bf16x4 w = *reinterpret_cast<const bf16x4 *>(wy + c);
+        bf16x4 o;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] = (bf16_t)((sum[dt][4 * q + r] * e.inv - e.t * (float)w[r]) * a.inv_n);
+        if (c + 4 <= a.d && (a.ld_dh & 3) == 0 && (reinterpret_cast<uintptr_t>(a.dh) & 7u) == 0) {
+          *reinterpret_cast<bf16x4 *>(dh + c) = o;
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (c + r < a.d) dh[c + r] = o[r];
+        }
+      }
+  }
+}
+
+// Joins the class ranges of 32 rows (a workgroup): each has its own maximum.
+template <int DP, bool GRAD>
+__global__ __launch_bounds__(256) void head_join_kernel(const RowsArgs a) {
+  const Meta &meta = *a.meta;
+  const int splits = meta.splits, row_tile = blockIdx.x >> 2, wave = blockIdx.x & 3;
+  if (splits == 1 || row_tile >= meta.row_tiles) return;
+  __shared__ float turned[32][DP + 1];
+  __shared__ float inv[32], ts[32];
+  __shared__ int label[32], row[32];
+  const int n = threadIdx.x & 31, g = threadIdx.x >> 5, i = row_tile * kOwned + wave * 32 + n;
+  const int64_t item0 = (int64_t)row_tile * splits;
+  const float *stat = a.part_stat + (size_t)item0 * 3 * kOwned + wave * 32 + n;
+  const int lab = a.label[i];
+  float m = kNoMax, others = 0.f, zl = -INFINITY;
+  for (int s = 0; s < splits; ++s) m = fmaxf(m, stat[(size_t)s * 3 * kOwned]);
+  for (int s = 0; s < splits; ++s) {
+    const float *p = stat + (size_t)s * 3 * kOwned;
+    others += p[kOwned] * exp_diff(p[0], m);
+    if (lab >= 0 && (lab / kTile) / meta.tiles_per == s) zl = p[2 * kOwned];
+  }
+  const RowEnd e = end_row(m, others, zl);
+  if (g == 0) {
+    const bool on = i < meta.n;
+    inv[n] = e.inv;
+    ts[n] = e.t;
+    label[n] = on ? lab : -1;
+    row[n] = on ? a.list[i] : -1;
+    if (on) {
+      a.row_loss[a.list[i]] = e.loss;
+      a.max[i] = m;
+      a.log[i] = e.log;
+      a.t[i] = e.t;
+    }
+  }
+  if (!GRAD || a.dh == nullptr) return;
+  for (int d0 = 0; d0 < DP; d0 += 8) {
+    float x = 0.f;
+    for (int s = 0; s < splits; ++s)
+      x += a.part[(((size_t)(item0 + s) * 4 + wave) * DP + d0 + g) * 32 + n] * exp_diff(stat[(size_t)s * 3 * kOwned], m);
+    turned[n][d0 + g] = x;
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < 32 * DP; k += 256) {
+    const int r = k / DP, c = k % DP;
+    if (label[r] >= 0 && c < a.d)
+      a.dh[(size_t)((int64_t)row[r] * a.ld_dh) + c] = (bf16_t)((turned[r][c] * inv[r] - ts[r] * (float)a.W[(size_t)label[r] * DP + c]) * a.inv_n);
+  }
+}
+
+struct ClassesArgs {
+  const Meta *meta;
+  const bf16_t *rows, *W;
+  const float *bias;
+  const float *stats;      // packed, of padded_rows each: maximum, -log2 sum, label (int), o / l
+  int64_t padded_rows;
+  int32_t C, d;
+  int32_t ranges;          // row ranges of the launch
+  float inv_n;
+  float *dW, *db;          // "+=" (one row range), either may be NULL
+  float *part;             // [range][d][ld_part]
+  float *part_db;          // [range][ld_part]
+  int32_t ld_part;
+};
+
+template <int DP, int IN_REGS>
+__global__ __launch_bounds__(256, 2) void head_classes_kernel(const ClassesArgs a) {
+  typedef Geometry<DP> G;
+  typedef Owned<DP, IN_REGS> Own;
+  struct Stats {
+    float max[kTile];
+    float log[kTile];
+    int32_t label[kTile];
+    float t[kTile];
+  };
+  __shared__ __attribute__((aligned(1024))) char tile0[G::tile_bytes];
+  __shared__ __attribute__((aligned(1024))) char tile1[G::tile_bytes];
+  __shared__ __attribute__((aligned(16))) Stats stats0;
+  __shared__ __attribute__((aligned(16))) Stats stats1;
+  __shared__ __attribute__((aligned(16))) char shared[Own::in_lds > 0 ? 4 * Own::in_lds * 1024 : 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  const Meta &meta = *a.meta;
+  const int range = blockIdx.x % a.ranges, class_tile = blockIdx.x / a.ranges;
+  if (range >= meta.ranges) return;
+  const int first = class_tile * kOwned + wave * 32, c = first + (lane & 31);
+  const bool idle = first >= a.C;  // this wave has no classes; it still loads
+  const Own own(a.W, first, wave, lane, shared);
+  const float bias = a.bias[c];
+  f32x16 sum[DP / 32];
+  clear<DP>(sum);
+  float g_sum = 0.f, g_low = 0.f;
+  Places<DP> at(wave, lane);
+  const int tiles = (meta.n + kTile - 1) / kTile, per = meta.rows_per / kTile, begin = range * per, end = min(tiles, begin + per);
+  auto load = [&](int tile, lds_char *dst, Stats *st) {
+    load_tile<DP>(a.rows + (size_t)tile * kTile * DP, dst, wave, at.load);
+    if (threadIdx.x < kTile)
+      load_lds16(a.stats + (size_t)(threadIdx.x >> 3) * a.padded_rows + (size_t)tile * kTile + (threadIdx.x & 7) * 4, (lds_char *)st);
+  };
+  auto step = [&](int tile, const lds_char *now, const Stats *st, lds_char *next, Stats *next_st) {
+    wait_tile();
+    if (tile + 1 < end) load(tile + 1, next, next_st);
+    if (idle) return;
+    at.renew();
+    // (the bias first, as in the rows kernel: the same logits to the last bit, so that large ones meet their own maximum)
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = bias;
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(first_operand<DP>(now, at.first, ks), own(ks), z, 0, 0, 0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 m = *reinterpret_cast<const f32x4 *>(st->max + 8 * q + 4 * h), l = *reinterpret_cast<const f32x4 *>(st->log + 8 * q + 4 * h);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[4 * q + r] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + r] - m[r], kLog2e, l[r]));
+    }
+    if (__any((uint32_t)(st->label[lane & 31] - first) < 32u)) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const i32x4 y = *reinterpret_cast<const i32x4 *>(st->label + 8 * q + 4 * h);
+        const f32x4 t = *reinterpret_cast<const f32x4 *>(st->t + 8 * q + 4 * h);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[4 * q + r] = y[r] == c ? -t[r] : z[4 * q + r];
+      }
+    }
+    // db takes g as it is; its long sum is compensated
+    float part = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) part += z[i];
+    const float y = part - g_low, s = g_sum + y;
+    g_low = (s - g_sum) - y;
+    g_sum = s;
+    bf16x8 high[2], low[2];  // g = high + low to 16 bits
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      high[i >> 3][i & 7] = (bf16_t)z[i];
+      low[i >> 3][i & 7] = (bf16_t)(z[i] - (float)high[i >> 3][i & 7]);
+    }
+#pragma unroll
+    for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8 x = second_operand<DP>(now, at.second, dt, t);
+        sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, high[t], sum[dt], 0, 0, 0);
+        sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, low[t], sum[dt], 0, 0, 0);
+      }
+  };
+  if (begin < end) load(begin, (lds_char *)tile0, &stats0);
+  for (int tile = begin; tile < end; tile += 2) {
+    step(tile, (const lds_char *)tile0, &stats0, (lds_char *)tile1, &stats1);
+    if (tile + 1 < end) step(tile + 1, (const lds_char *)tile1, &stats1, (lds_char *)tile0, &stats0);
+  }
+  if (c >= a.C) return;
+  g_sum += __shfl_xor(g_sum, 32);
+  const bool whole = a.ranges == 1;
+  if (a.db != nullptr && h == 0) {
+    if (whole)
+      a.db[c] += g_sum * a.inv_n;
+    else
+      a.part_db[(size_t)range * a.ld_part + c] = g_sum;
+  }
+  if (a.dW == nullptr) return;
+#pragma unroll
+  for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+      const int k = 32 * dt + 8 * (t >> 2) + 4 * h + (t & 3);
+      if (k >= a.d) continue;
+      if (whole)
+        a.dW[(size_t)k * a.C + c] += sum[dt][t] * a.inv_n;
+      else
+        a.part[((size_t)range * a.d + k) * a.ld_part + c] = sum[dt][t];
+    }
+}
+
+// dW[k][c] += inv_n * sum over the row ranges, in their order; row d is db.  64 outputs per workgroup, four runs of ranges side by side.
+__global__ __launch_bounds__(256) void head_reduce_kernel(const ClassesArgs a) {
+  __shared__ float red[4][64];
+  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6, ranges = a.meta->ranges, k = blockIdx.y;
+  const int c = blockIdx.x * 64 + tx;
+  const bool bias = k == a.d;
+  float *dst = bias ? a.db : a.dW == nullptr ? nullptr : a.dW + (size_t)k * a.C;
+  if (dst == nullptr) return;  // whole workgroup
+  const float *src = bias ? a.part_db : a.part + (size_t)k * a.ld_part;
+  const size_t stride = bias ? (size_t)a.ld_part : (size_t)a.d * a.ld_part;
+  const int per = (ranges + 3) / 4, r0 = ty * per, r1 = min(ranges, r0 + per);
+  float s = 0.f;
+  if (c < a.C) {
+    int r = r0;
+    for (; r + 8 <= r1; r += 8) {
+      float v[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) v[t] = src[(size_t)(r + t) * stride + c];
+      s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    }
+    for (; r < r1; ++r) s += src[(size_t)r * stride + c];
+  }
+  red[ty][tx] = s;
+  __syncthreads();
+  if (ty == 0 && c < a.C) dst[c] += a.inv_n * ((red[0][tx] + red[1][tx]) + (red[2][tx] + red[3][tx]));
+}
+
+struct PrepareArgs {
+  const bf16_t *h, *W;
+  int64_t ld_h;
+  const float *bias_in;
+  const int32_t *labels;
+  const uint8_t *mask;
+  int64_t rows;
+  int32_t d, C, DP, padded_classes;
+  int32_t *counts;        // labelled rows of every kMetaBlock
+  int32_t n_counts;
+  Meta *meta;
+  int32_t *list;
+  int64_t padded_rows;
+  bf16_t *packed, *Wt;
+  float *bias;
+  float *stats;           // maximum, -log2 sum, label, t
+  float *row_loss;
+  bf16_t *dh;
+  int64_t ld_dh;
+  int32_t max_splits, ranges;
+};
+
+// Workgroups [0, n_counts) count labelled rows; the others turn the weights, 64 x 64 at a time, and pad the biases.
+__global__ __launch_bounds__(256) void head_count_kernel(const PrepareArgs a) {
+  __shared__ bf16_t turned[64][66];
+  __shared__ int total;
+  if ((int)blockIdx.x < a.n_counts) {
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    const int64_t r0 = (int64_t)blockIdx.x * kMetaBlock;
+    int count = 0;
+    for (int i = threadIdx.x; i < kMetaBlock; i += 256) {
+      const bool on = r0 + i < a.rows && is_labelled(a.labels, a.mask, r0 + i, a.C);
+      count += __popcll(__ballot(on));  // the wave's
+    }
+    if ((threadIdx.x & 63) == 0) atomicAdd(&total, count);
+    __syncthreads();
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = total;
+    return;
+  }
+  const int tk = a.DP / 64, block = blockIdx.x - a.n_counts, k0 = block % tk * 64, c0 = block / tk * 64;
+  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+  if (k0 == 0 && threadIdx.x < 64) {
+    const int c = c0 + threadIdx.x;
+    float b = -INFINITY;
+    if (c < a.C) b = a.bias_in == nullptr ? 0.f : a.bias_in[c];
+    a.bias[c] = b;
+  }
+#pragma unroll
+  for (int i = 0; i < 64; i += 4) {
+    const int k = k0 + y + i, c = c0 + x;
+    turned[x][y + i] = k < a.d && c < a.C ? a.W[(size_t)k * a.C + c] : (bf16_t)0.f;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 64; i += 4) a.Wt[(size_t)(c0 + y + i) * a.DP + k0 + x] = turned[y + i][x];
+}
+
+// The list of labelled rows, in their order; what hangs on their number.
+__global__ __launch_bounds__(256) void head_list_kernel(const PrepareArgs a) {
+  __shared__ int before, in_wave[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (threadIdx.x == 0) before = 0;
+  __syncthreads();
+  int mine = 0;
+  for (int i = threadIdx.x; i < (int)blockIdx.x; i += 256) mine += a.counts[i];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o);
+  if (lane == 0) atomicAdd(&before, mine);
+  __syncthreads();
+  int at = before;
+  const int64_t r0 = (int64_t)blockIdx.x * kMetaBlock;
+  int32_t *label = reinterpret_cast<int32_t *>(a.stats + 2 * a.padded_rows);
+  for (int i = 0; i < kMetaBlock; i += 256) {
+    const int64_t r = r0 + i + threadIdx.x;
+    const bool in = r < a.rows, on = in && is_labelled(a.labels, a.mask, r, a.C);
+    const uint64_t votes = __ballot(on);
+    if (lane == 0) in_wave[wave] = __popcll(votes);
+    __syncthreads();
+    int pos = at + __popcll(votes & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) pos += in_wave[w];
+    if (on) {
+      a.list[pos] = (int32_t)r;
+      label[pos] = a.labels[r];
+    } else if (in) {
+      a.row_loss[r] = 0.f;
+    }
+    at += in_wave[0] + in_wave[1] + in_wave[2] + in_wave[3];
+    __syncthreads();
+  }
+  if ((int)blockIdx.x == a.n_counts - 1 && threadIdx.x == 0) {
+    Meta m{};
+    m.n = at;
+    m.row_tiles = (at + kOwned - 1) / kOwned;
+    // class ranges: as many as make the last round of workgroups a full one.  A range costs its tiles and about eight more (its
+    // rows, its partial sums and their reading).
+    const int tiles = (a.C + kTile - 1) / kTile;
+    int64_t best = -1;
+    for (int s = 1; s <= a.max_splits && m.row_tiles > 0; ++s) {
+      const int per = (tiles + s - 1) / s, real = (tiles + per - 1) / per;
+      const int64_t items = (int64_t)m.row_tiles * real, cost = (items + kRound - 1) / kRound * (per + (real > 1 ? 8 : 4));
+      if (real > 1 && items > kRowItems) break;
+      if (best < 0 || cost < best) {
+        best = cost;
+        m.splits = real;
+        m.tiles_per = per;
+      }
+    }
+    if (m.splits == 0) {
+      m.splits = 1;
+      m.tiles_per = tiles;
+    }
+    const int row_steps = (at + kTile - 1) / kTile, per = (row_steps + a.ranges - 1) / a.ranges;
+    m.rows_per = max(per, 1) * kTile;
+    m.ranges = (row_steps + max(per, 1) - 1) / max(per, 1);
+    *a.meta = m;
+  }
+}
+
+// The labelled rows side by side, zeros from d to DP and behind the last of them up to whole workgroups; zero rows of dh for the others.
+// A thread per eight columns.
+__global__ __launch_bounds__(256) void head_pack_kernel(const PrepareArgs a, int64_t pack_blocks) {
+  const int per_row = a.DP / 8;
+  if ((int64_t)blockIdx.x < pack_blocks) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / per_row;
+    const int k = (threadIdx.x % per_row) * 8, n = a.meta->n;
+    if (i >= (int64_t)(n + kOwned - 1) / kOwned * kOwned) return;
+    bf16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (i < n) {
+      const bf16_t *src = a.h + (size_t)(a.list[i] * a.ld_h) + k;
+      if (k + 8 <= a.d && (a.ld_h & 7) == 0 && (reinterpret_cast<uintptr_t>(a.h) & 15u) == 0) {
+        v = *reinterpret_cast<const bf16x8 *>(src);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if (k + t < a.d) v[t] = src[t];
+      }
+    } else if (k == 0) {
+      a.stats[i] = INFINITY;
+      reinterpret_cast<int32_t *>(a.stats + 2 * a.padded_rows)[i] = -1;
+      a.stats[a.padded_rows + i] = a.stats[3 * a.padded_rows + i] = 0.f;
+    }
+    *reinterpret_cast<bf16x8 *>(a.packed + (size_t)i * a.DP + k) = v;
+    return;
+  }
+  const int64_t i = (((int64_t)blockIdx.x - pack_blocks) * 256 + threadIdx.x) / per_row;
+  const int k = (threadIdx.x % per_row) * 8;
+  if (i >= a.rows || k >= a.d || is_labelled(a.labels, a.mask, i, a.C)) return;
+  bf16_t *dst = a.dh + (size_t)(i * a.ld_dh) + k;
+  if (k + 8 <= a.d && (a.ld_dh & 7) == 0 && (reinterpret_cast<uintptr_t>(a.dh) & 15u) == 0) {
+    *reinterpret_cast<bf16x8 *>(dst) = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      if (k + t < a.d) dst[t] = (bf16_t)0.f;
+  }
+}
+
+struct FusedPlan {
+  int64_t rows = 0, padded_rows = 0, max_items = 0, pack_blocks = 0;
+  int d = 0, C = 0, DP = 0, padded_classes = 0, n_counts = 0, max_splits = 1, ranges = 1, class_tiles = 0, ld_part = 0;
+  bool grads = false;
+  size_t counts = 0, meta = 0, list = 0, stats = 0, packed = 0, Wt = 0, bias = 0, part = 0, part_stat = 0, part_dW = 0, part_db = 0, total = 0;
+};
+constexpr int64_t kFusedRows = (int64_t)1 << 20;  // of a slab: their packed copy is half a gigabyte at most
+constexpr size_t kRangeBytes = (size_t)256 << 20;  // partial sums of the classes kernel
+
+bool fused_takes(int d, int dtype) { return dtype == GNNSTAGE_BF16 && d <= 256; }
+
+FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads) {
+  FusedPlan p;
+  const int64_t rows = std::min(all_rows, kFusedRows);
+  p.rows = rows;
+  p.d = d;
+  p.C = C;
+  p.grads = grads;
+  p.DP = d <= 64 ? 64 : d <= 128 ? 128 : 256;
+  const int64_t row_tiles = std::max<int64_t>(1, (rows + kOwned - 1) / kOwned);
+  p.padded_rows = row_tiles * kOwned;
+  p.class_tiles = (C + kOwned - 1) / kOwned;
+  p.padded_classes = p.class_tiles * kOwned;
+  p.n_counts = (int)std::max<int64_t>(1, (rows + kMetaBlock - 1) / kMetaBlock);
+  p.pack_blocks = p.padded_rows * (p.DP / 8) / 256;
+  // class ranges of eight tiles at least
+  p.max_splits = std::max(1, std::min(64, (C + 8 * kTile - 1) / (8 * kTile)));
+  p.max_items = std::min(row_tiles * p.max_splits, std::max<int64_t>(row_tiles, kRowItems));
+  // row ranges of the classes kernel: rounds of workgroups filled as far as the partial sums' room allows
+  const int64_t steps = std::max<int64_t>(1, (rows + kTile - 1) / kTile);
+  p.ld_part = round_up(C, 32);
+  const size_t bytes = sizeof(float) * (size_t)d * p.ld_part;
+  double best = -1;
+  for (int r = 1; r <= 512 && r <= steps && (r == 1 || (size_t)r * bytes <= kRangeBytes); ++r) {
+    const int64_t items = (int64_t)p.class_tiles * r;
+    const int64_t per = (steps + r - 1) / r;
+    const double cost = (double)((items + kRound - 1) / kRound) * (double)(per + (r > 1 ? 8 : 4));
+    if (best < 0 || cost < best) {
+      best = cost;
+      p.ranges = r;
+    }
+  }
+  size_t off = 0;
+  auto take = [&](size_t b) {
+    const size_t at = off;
+    off = align256(off + b);
+    return at;
+  };
+  p.counts = take(sizeof(int32_t) * (size_t)p.n_counts);
+  p.meta = take(sizeof(Meta));
+  p.list = take(sizeof(int32_t) * (size_t)p.padded_rows);
+  p.stats = take(4 * sizeof(float) * (size_t)p.padded_rows);
+  p.packed = take(2 * (size_t)p.padded_rows * p.DP);
+  p.Wt = take(2 * (size_t)p.padded_classes * p.DP);
+  p.bias = take(sizeof(float) * (size_t)p.padded_classes);
+  const int64_t part_items = p.max_splits > 1 ? std::min<int64_t>(p.max_items, kRowItems) : 0;
+  p.part_stat = take(sizeof(float) * 3 * kOwned * (size_t)part_items);
+  p.part = take(grads ? sizeof(float) * (size_t)kOwned * p.DP * (size_t)part_items : 0);
+  p.part_dW = take(grads && p.ranges > 1 ? bytes * (size_t)p.ranges : 0);
+  p.part_db = take(grads && p.ranges > 1 ? sizeof(float) * (size_t)p.ld_part * p.ranges : 0);
+  p.total = off;
+  return p;
+}
+
+// Owned operands in registers, of d / 16: all of them where the registers reach.
+constexpr int kRowsInRegs = 12, kClassesInRegs = 8;  // width 256
+
+// a slab of at most p.rows rows; first: the weights are not there yet
+template <int DP>
+int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipStream_t s) {
+  auto at = [&](size_t off) { return c.ws + off; };
+  PrepareArgs a{};
+  a.h = static_cast<const bf16_t *>(c.h);
+  a.W = static_cast<const bf16_t *>(c.W);
+  a.ld_h = c.ld_h;
+  a.bias_in = c.bias;
+  a.labels = c.labels;
+  a.mask = c.mask;
+  a.rows = rows;
+  a.d = p.d;
+  a.C = p.C;
+  a.DP = DP;
+  a.padded_classes = p.padded_classes;
+  a.counts = reinterpret_cast<int32_t *>(at(p.counts));
+  a.n_counts = (int)((rows + kMetaBlock - 1) / kMetaBlock);
+  a.meta = reinterpret_cast<Meta *>(at(p.meta));
+  a.list = reinterpret_cast<int32_t *>(at(p.list));
+  a.padded_rows = p.padded_rows;
+  a.packed = reinterpret_cast<bf16_t *>(at(p.packed));
+  a.Wt = reinterpret_cast<bf16_t *>(at(p.Wt));
+  a.bias = reinterpret_cast<float *>(at(p.bias));
+  a.stats = reinterpret_cast<float *>(at(p.stats));
+  a.row_loss = c.row_loss;
+  a.dh = static_cast<bf16_t *>(c.dh);
+  a.ld_dh = c.ld_dh;
+  a.max_splits = p.max_splits;
+  a.ranges = p.ranges;
+  const unsigned turn_blocks = first ? (unsigned)(p.padded_classes / 64 * (DP / 64)) : 0;
+  hipLaunchKernelGGL(head_count_kernel, dim3((unsigned)a.n_counts + turn_blocks), dim3(256), 0, s, a);
+  HEAD_TRY(hipGetLastError());
+  hipLaunchKernelGGL(head_list_kernel, dim3((unsigned)a.n_counts), dim3(256), 0, s, a);
+  HEAD_TRY(hipGetLastError());
+  const int64_t zero_blocks = c.dh ? (rows * (DP / 8) + 255) / 256 : 0;
+  hipLaunchKernelGGL(head_pack_kernel, dim3((unsigned)(p.pack_blocks + zero_blocks)), dim3(256), 0, s, a, p.pack_blocks);
+  HEAD_TRY(hipGetLastError());
+
+  RowsArgs r{};
+  r.meta = a.meta;
+  r.rows = a.packed;
+  r.W = a.Wt;
+  r.bias = a.bias;
+  r.label = reinterpret_cast<const int32_t *>(a.stats + 2 * p.padded_rows);
+  r.list = a.list;
+  r.C = p.C;
+  r.d = p.d;
+  r.inv_n = c.inv_n;
+  r.row_loss = c.row_loss;
+  r.dh = a.dh;
+  r.ld_dh = c.ld_dh;
+  r.max = a.stats;
+  r.log = a.stats + p.padded_rows;
+  r.t = a.stats + 3 * p.padded_rows;
+  r.part = reinterpret_cast<float *>(at(p.part));
+  r.part_stat = reinterpret_cast<float *>(at(p.part_stat));
+  constexpr int kAll = DP / 16;
+  const bool sums = c.dh != nullptr;
+  hipLaunchKernelGGL((sums ? head_rows_kernel<DP, true, (kAll < kRowsInRegs ? kAll : kRowsInRegs)> : head_rows_kernel<DP, false, kAll>),
+                     dim3((unsigned)p.max_items), dim3(256), 0, s, r);
+  HEAD_TRY(hipGetLastError());
+  if (p.max_splits > 1) {
+    const unsigned blocks = 4u * (unsigned)std::min<int64_t>(p.padded_rows / kOwned, kRowItems);
+    hipLaunchKernelGGL((sums ? head_join_kernel<DP, true> : head_join_kernel<DP, false>), dim3(blocks), dim3(256), 0, s, r);
+    HEAD_TRY(hipGetLastError());
+  }
+  if (!c.dW && !c.db) return hipSuccess;
+  ClassesArgs k{};
+  k.meta = a.meta;
+  k.rows = a.packed;
+  k.W = a.Wt;
+  k.bias = a.bias;
+  k.stats = a.stats;
+  k.padded_rows = p.padded_rows;
+  k.C = p.C;
+  k.d = p.d;
+  k.ranges = p.ranges;
+  k.inv_n = c.inv_n;
+  k.dW = c.dW;
+  k.db = c.db;
+  k.part = reinterpret_cast<float *>(at(p.part_dW));
+  k.part_db = reinterpret_cast<float *>(at(p.part_db));
+  k.ld_part = p.ld_part;
+  hipLaunchKernelGGL((head_classes_kernel<DP, (kAll < kClassesInRegs ? kAll : kClassesInRegs)>), dim3((unsigned)(p.class_tiles * p.ranges)),
+                     dim3(256), 0, s, k);
+  HEAD_TRY(hipGetLastError());
+  if (p.ranges > 1) {
+    hipLaunchKernelGGL(head_reduce_kernel, dim3((unsigned)((p.C + 63) / 64), (unsigned)p.d + 1), dim3(256), 0, s, k);
+    HEAD_TRY(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+size_t workspace_bytes_of(const Plan &p) {
+  return fused_takes(p.d, p.dtype) ? fused_plan(p.rows, p.d, p.C, p.grads).total : p.total;
+}
+
 }  // namespace
 
 extern "C" size_t gnntrain_head_xent_workspace_size(int64_t rows, int32_t d, int32_t n_classes, int32_t dtype, int32_t want_grads) try {
@@ -338,7 +1164,7 @@ extern "C" size_t gnntrain_head_xent_workspace_size(int64_t rows, int32_t d, int
     train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: " + err);
     return 0;
   }
-  return p.total;
+  return workspace_bytes_of(p);
 }
 GNNSTAGE_GUARD_SIZE
 
@@ -353,9 +1179,25 @@ extern "C" int gnntrain_head_xent(const void *h, int64_t ld_h, const void *W, in
   if (rows == 0) return GNNSTAGE_OK;
   if (!h || !W || !labels || !row_loss) return train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: h, W, labels and row_loss must not be NULL");
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: workspace must be 256-byte aligned");
-  if (workspace_bytes < p.total) return train_error(GNNSTAGE_ENOMEM, "gnntrain_head_xent: workspace smaller than gnntrain_head_xent_workspace_size()");
+  if (workspace_bytes < workspace_bytes_of(p)) return train_error(GNNSTAGE_ENOMEM, "gnntrain_head_xent: workspace smaller than gnntrain_head_xent_workspace_size()");
   const Call c{h, ld_h, W, bias, labels, mask, inv_n_train, row_loss, dh, ld_dh, dW, db, static_cast<char *>(workspace)};
-  const int e = run_in_pieces(p, c, static_cast<hipStream_t>(hip_stream));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  int e = hipSuccess;
+  if (fused_takes(d, dtype)) {
+    const FusedPlan f = fused_plan(rows, d, n_classes, grads);
+    for (int64_t r = 0; r < rows && e == hipSuccess; r += f.rows) {
+      Call slab = c;
+      slab.h = static_cast<const bf16_t *>(h) + (size_t)(r * ld_h);
+      slab.labels = labels + r;
+      slab.mask = mask ? mask + r : nullptr;
+      slab.row_loss = row_loss + r;
+      slab.dh = dh ? static_cast<bf16_t *>(dh) + (size_t)(r * ld_dh) : nullptr;
+      const int64_t m = std::min(f.rows, rows - r);
+      e = f.DP == 64 ? run_fused<64>(f, slab, m, r == 0, s) : f.DP == 128 ? run_fused<128>(f, slab, m, r == 0, s) : run_fused<256>(f, slab, m, r == 0, s);
+    }
+  } else {
+    e = run_in_pieces(p, c, s);
+  }
   if (e != hipSuccess) return train_error(GNNSTAGE_EHIP, std::string("gnntrain_head_xent: ") + hipGetErrorString((hipError_t)e));
   return GNNSTAGE_OK;
 }

@@ -180,6 +180,35 @@ def test_classes_left_out_by_their_bias(dtype, lowest):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bias", [-3.4028234663852886e38, 1e30, -1e9, 3e8])
+def test_all_classes_at_a_bias_beyond_every_logit(dtype, bias):
+    """All logits are the bias then, a step of fp32 above what products add: the softmax is flat, and a large logit is its own maximum."""
+    h, W, b, y, mask = head_inputs(50, 48, 300, dtype, 12, "all")
+    got = run_head(h * 2.0 ** -10, W, np.full_like(b, bias), y, mask, 1.0, dtype)
+    assert np.abs(got["loss"] - np.log(300.0)).max() <= 1e-5
+    assert np.abs(got["db"].sum()) <= 1e-3 and np.isfinite(got["dW"]).all() and np.isfinite(got["dh"]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1e3, 1e7, 1e18])
+def test_large_logits_stay_numbers(dtype, scale):
+    """Logits so large that every row is sure of some class: the loss is the difference of two of them, and the gradient one-hot."""
+    h, W, b, y, mask = head_inputs(70, 64, 200, dtype, 13, "all", lean=0.0)
+    h, W = (h.float() * scale).to(DT[dtype]), (W.float() * scale).to(DT[dtype])
+    got = run_head(h, W, np.zeros_like(b), y, mask, 1.0, dtype)
+    z = h.double().numpy() @ W.double().numpy()
+    top = z.max(1)
+    second = np.sort(z, 1)[:, -2]
+    mag = (np.abs(h.double().numpy()) @ np.abs(W.double().numpy())).max(1)
+    own = z[np.arange(70), y]
+    off = np.abs(got["loss"] - (top - own))
+    clear = (top - second) > 40 + 8 * 66 * U * mag  # rows whose largest logit leads in any order of additions
+    assert clear.sum() >= 40
+    assert np.all(off[clear] <= (2 * 66 * U * mag + U * np.abs(top - own) + 1e-6)[clear])
+    assert np.isfinite(got["dh"]).all() and np.isfinite(got["dW"]).all() and np.isfinite(got["db"]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_row_whose_label_is_left_out(dtype):
     def edit(h, W, b, y, mask):
         b[5] = -np.inf
