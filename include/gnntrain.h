@@ -70,11 +70,13 @@ typedef struct {
                            come from gnnstage_level_buffers */
   void *workspace;    /* DEVICE, 256-byte aligned, >= gnntrain_workspace_size() bytes */
   size_t workspace_bytes;
+  int32_t head_fused; /* non-zero: the head is gnntrain_head_xent, which keeps neither logits nor their gradients; n_classes may then be up to
+                         2^24 (otherwise 65,536) */
 } gnntrain_desc;
 
 /* Device bytes the loop needs: optimiser moments, logits of up to 131,072 vertices, gradient of the logits and
  * gradient rows of the last level for all vertices, per-vertex losses, staged head weights, split-reduction
- * scratch.  Host-only; 0 on an invalid descriptor. */
+ * scratch (head_fused: gnntrain_head_xent's workspace in the place of logits, their gradients, weights and scratch).  Host-only; 0 on an invalid descriptor. */
 size_t gnntrain_workspace_size(const gnntrain_desc *desc);
 
 /* Validates the descriptor against the stage handles (chaining of the level buffers, label range),

@@ -39,7 +39,7 @@ class gnnstage_desc(C.Structure):
         ("grad_in", C.c_void_p), ("grad_h0", C.c_void_p), ("need_input_grad", C.c_int32),
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
         ("ln_gamma", C.c_void_p), ("ln_beta", C.c_void_p), ("d_ln_gamma", C.c_void_p), ("d_ln_beta", C.c_void_p),
-        ("ln_eps", C.c_float), ("dropout_p", C.c_float),
+        ("ln_eps", C.c_float), ("dropout_p", C.c_float), ("save_8bit", C.c_int32),
     ]
 
 
@@ -57,7 +57,7 @@ class gnntrain_desc(C.Structure):
         ("optimizer", C.c_int32), ("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
         ("weight_decay", C.c_float),
         ("shuffle", C.c_int32), ("seed", C.c_uint64), ("alpha_hist", C.c_int32), ("history_swap", C.c_int32),
-        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("head_fused", C.c_int32),
     ]
 
 
@@ -499,7 +499,8 @@ def gnnstage_rows8_weight_grad(q, scale, dY, dW, workspace, dbias=None) -> None:
 
 
 class GnnStage:
-    """A stage handle plus the tensors it points at.
+    """A stage handle plus the tensors it points at.  ``save_8bit``: what the forward pass saves for the weight gradients
+    is kept in 8 bits.
 
     ``cur`` / ``hist`` / ``W`` / ``bias`` / ``dW`` / ``dbias`` are lists of CUDA(HIP) tensors owned by
     the caller; the workspace is allocated here with ``torch.empty`` (device memory only).
@@ -508,7 +509,7 @@ class GnnStage:
     def __init__(self, row_ptr, col_idx, chunk_ptr, dims, *, W, cur, hist, dW, bias=None, dbias=None,
                  edge_val=None, variant=GNNSTAGE_GCN, alpha=0.0, beta=None, h0=None, grad_h0=None,
                  dtype=GNNSTAGE_F32, level0_f32=False, grad_in=None, device="cuda:0", ln_gamma=None, ln_beta=None,
-                 d_ln_gamma=None, d_ln_beta=None, ln_eps=1e-5, dropout_p=0.0):
+                 d_ln_gamma=None, d_ln_beta=None, ln_eps=1e-5, dropout_p=0.0, save_8bit=False):
         import torch
 
         self._torch = torch
@@ -548,6 +549,7 @@ class GnnStage:
         d.ln_gamma, d.ln_beta, d.d_ln_gamma, d.d_ln_beta = (vp(x) for x in self._keep_ln)
         d.ln_eps = float(ln_eps)
         d.dropout_p = float(dropout_p)
+        d.save_8bit = int(bool(save_8bit))
         size = int(lib.gnnstage_workspace_size(C.byref(d)))
         if size == 0:
             raise GnnStageError(-1, lib.gnnstage_last_error(None).decode())
@@ -789,11 +791,12 @@ def gnntrain_sgd_step(p, g, compute, lr, weight_decay) -> None:
 
 class GnnTrainer:
     """Handle of the epoch loop plus the tensors it points at.  ``params`` is a list of
-    ``(master fp32 tensor, compute tensor or None, grad fp32 tensor)``."""
+    ``(master fp32 tensor, compute tensor or None, grad fp32 tensor)``.  ``head_fused``: the loss head keeps no logits
+    (gnntrain_head_xent)."""
 
     def __init__(self, stages: Sequence["GnnStage"], *, head_W, head_b, head_dW, head_db, labels, train_mask, params,
                  optimizer=GNNTRAIN_ADAM, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, shuffle=True,
-                 seed=0, alpha_hist=1, history_swap=False, device="cuda:0"):
+                 seed=0, alpha_hist=1, history_swap=False, device="cuda:0", head_fused=False):
         import torch
 
         self._torch = torch
@@ -819,6 +822,7 @@ class GnnTrainer:
         d.weight_decay = float(weight_decay)
         d.shuffle, d.seed, d.alpha_hist = int(bool(shuffle)), int(seed), int(alpha_hist)
         d.history_swap = int(bool(history_swap))
+        d.head_fused = int(bool(head_fused))
         size = int(lib.gnntrain_workspace_size(C.byref(d)))
         if size == 0:
             raise GnnStageError(-1, "gnntrain_workspace_size: invalid descriptor")

@@ -391,6 +391,7 @@ struct Layout {
   size_t ln_stride;            // of the parameter sums of one layer
   int ln_layers;               // layers whose parameter sums wait to be added up at a time
   std::vector<size_t> Z, dZ, Wt, Wn, Tc, Th;
+  std::vector<size_t> Z8, Z8s;  // save_8bit: the saved aggregations and their factors; Z[j] is then borrowed room for the forward layer alone
   std::vector<size_t> dY;  // deferred weight gradients: dL/d(pre-activation) of every aggregate-first layer, all n rows
   std::vector<size_t> Wt_self, Wn_self;  // GraphSage: staged copies of W_self (Wt / Wn then hold W_neigh)
   size_t self_fwd = 0, self_bwd = 0;      // GraphSage: h_v W_self (fp32), dY W_self^T where it can't wait in the output rows
@@ -407,6 +408,8 @@ struct Shape {
   std::vector<int> dims, ld;
   std::vector<char> tf;  // per layer: 1 = transform first (gather rows of width d_{j+1}), 0 = aggregate first
   int dtype = 0, level0_f32 = 0, variant = 0, need_input_grad = 0;
+  bool save8 = false;
+  int ld8(int j) const { return round_up(dims[j], 32); }  // of a row kept in 8 bits
   Tuning tune;
   bool has_bias() const { return variant != GNNSTAGE_GCNII; }
   // One weight-gradient product per layer over all rows at the end of the backward pass instead of one per chunk
@@ -506,6 +509,7 @@ bool read_shape(const gnnstage_desc *d, Shape &s, std::string &err) {
   s.level0_f32 = (d->dtype == GNNSTAGE_BF16 && d->level0_f32) ? 1 : 0;
   s.variant = d->variant;
   s.need_input_grad = d->need_input_grad ? 1 : 0;
+  s.save8 = d->save_8bit != 0;
   s.chunk_ptr.assign(d->chunk_ptr, d->chunk_ptr + s.K + 1);
   if (s.chunk_ptr[0] != 0 || s.chunk_ptr[s.K] != s.n) { err = "chunk_ptr must start at 0 and end at n_vertices"; return false; }
   for (int c = 0; c < s.K; ++c)
@@ -541,6 +545,32 @@ bool read_shape(const gnnstage_desc *d, Shape &s, std::string &err) {
   for (int64_t v = 0; v < s.n; ++v)
     if (d->row_ptr[v] > d->row_ptr[v + 1]) { err = "row_ptr must be non-decreasing"; return false; }
   return true;
+}
+
+// Saved aggregations in 8 bits.  A layer's aggregation is then needed as it is by the layer's own transform alone: it borrows
+// rows that only the backward pass uses, the widest of the gradient rows (dZ of any layer); where no layer's are wide enough it gets room
+// of its own, one for all layers.
+void save_in_8_bits(const Shape &s, Layout &l, Bump &w) {
+  l.Z8.assign(s.L, 0);
+  l.Z8s.assign(s.L, 0);
+  size_t at = 0;
+  int width = 0, need = 0;
+  for (int j = 0; j < s.L; ++j) {
+    const bool there = s.res() || s.tf[j] || j > 0 || s.need_input_grad;
+    const int ld = s.tf[j] ? s.ld[j + 1] : s.ld[j];
+    if (there && ld > width) {
+      width = ld;
+      at = l.dZ[j];
+    }
+    if (!s.tf[j]) need = std::max(need, s.ld[j]);
+  }
+  if (need > width) at = w.take((size_t)s.n * need * s.elt());
+  for (int j = 0; j < s.L; ++j) {
+    if (s.tf[j]) continue;
+    l.Z[j] = at;
+    l.Z8[j] = w.take((size_t)s.n * s.ld8(j));
+    l.Z8s[j] = w.take((size_t)s.n * (s.ld8(j) / 32));
+  }
 }
 
 Layout layout_for(const Shape &s, const HostDir &hf, const HostDir &hb, bool rank1, int64_t item_cap, int64_t slot_cap) {
@@ -623,7 +653,7 @@ Layout layout_for(const Shape &s, const HostDir &hf, const HostDir &hb, bool ran
     // gradient of the aggregation for ALL rows (the parameter gradient through historical rows needs it)
     l.Tc[j] = w.take((size_t)s.n * s.ld[j] * elt);
     l.Th[j] = w.take((size_t)s.n * s.ld[j] * elt);
-    l.Z[j] = w.take((size_t)s.n * s.ld[j] * elt);
+    l.Z[j] = s.save8 ? 0 : w.take((size_t)s.n * s.ld[j] * elt);
     l.dZ[j] = w.take((size_t)s.n * s.ld[j] * elt);
     // deferred weight gradients keep dY of all rows in the table of activated current rows (of the same width): a chunk's rows
     // of that table are written before they are read in a forward pass, and no backward pass reads them.  The gradient of the
@@ -639,11 +669,12 @@ Layout layout_for(const Shape &s, const HostDir &hf, const HostDir &hb, bool ran
       l.Th[j] = w.take((size_t)s.n * s.ld[j + 1] * elt);
       l.dZ[j] = w.take((size_t)s.n * s.ld[j + 1] * elt);
     } else {
-      l.Z[j] = w.take((size_t)s.n * s.ld[j] * elt);
+      l.Z[j] = s.save8 ? 0 : w.take((size_t)s.n * s.ld[j] * elt);
       l.dZ[j] = (j == 0 && !s.need_input_grad) ? 0 : w.take((size_t)s.n * s.ld[j] * elt);
       if (s.defer_wgrad()) l.dY[j] = w.take((size_t)s.n * s.ld[j + 1] * elt);
     }
   }
+  if (s.save8) save_in_8_bits(s, l, w);
   for (int j = 0; j < s.L; ++j) {
     l.Wt[j] = w.take((size_t)s.dims[j + 1] * s.ld[j] * elt);
     l.Wn[j] = w.take((size_t)s.dims[j] * s.ld[j + 1] * elt);
@@ -1329,6 +1360,10 @@ int forward_layer(gnnstage *st, int j, const Span &sp, hipStream_t stream) {
     if (st->output_dropout()) g.drop = st->dropout(j, r);
     HIP_TRY(st, launch_gemm_nt(g, cd, stream));
   }
+  if (s.save8)
+    HIP_TRY(st, launch_rows8_store(st->at<char>(st->lay.Z[j]) + (size_t)row0 * s.ld[j] * celt, cd, s.ld[j], M, s.dims[j],
+                                   st->at<int8_t>(st->lay.Z8[j]) + (size_t)row0 * s.ld8(j), s.ld8(j),
+                                   st->at<uint8_t>(st->lay.Z8s[j]) + (size_t)row0 * (s.ld8(j) / 32), s.ld8(j) / 32, stream));
   return GNNSTAGE_OK;
 }
 
@@ -1339,6 +1374,13 @@ void wgrad_products(gnnstage *st, int j, int64_t r0, int64_t M, const char *dY, 
   GemmTnArgs w = tn_args(st, st->at<char>(st->lay.Z[j]) + (size_t)r0 * s.ld[j] * s.elt(), cd, s.ld[j], dY, s.ld[j + 1], M, s.dims[j], s.dims[j + 1],
                          s.variant == GNNSTAGE_GCNII ? st->beta[j] : 1.f,
                          st->dW[j] + (s.sage() ? s.w_half(j) : 0));  // GraphSage: W_neigh is the lower half
+  if (s.save8) {
+    w.A = st->at<int8_t>(st->lay.Z8[j]) + (size_t)r0 * s.ld8(j);
+    w.a_dtype = DT_ROWS8;
+    w.lda = s.ld8(j);
+    w.a_scale = st->at<uint8_t>(st->lay.Z8s[j]) + (size_t)r0 * (s.ld8(j) / 32);
+    w.ld_scale = s.ld8(j) / 32;
+  }
   if (s.has_bias()) {
     w.dbias = st->dbias[j];
     w.bias_partial = st->at<float>(st->lay.bias_partial);

@@ -632,34 +632,51 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(const RowsArgs a) {
   }
 }
 
-// Joins the class ranges of 32 rows (a workgroup): each has its own maximum.
+// Joins the class ranges of 32 rows and 16 columns (a workgroup): each range has its own maximum.
+constexpr int kMaxSplits = 64;
+constexpr int kJoinColumns = 16;
 template <int DP, bool GRAD>
 __global__ __launch_bounds__(256) void head_join_kernel(const RowsArgs a) {
   const Meta &meta = *a.meta;
-  const int splits = meta.splits, row_tile = blockIdx.x >> 2, wave = blockIdx.x & 3;
+  const int splits = meta.splits, row_tile = blockIdx.x >> 2, wave = blockIdx.x & 3, d0 = blockIdx.y * kJoinColumns;
   if (splits == 1 || row_tile >= meta.row_tiles) return;
-  __shared__ float turned[32][DP + 1];
+  __shared__ float stat[3][kMaxSplits][32], red[8][32];
+  __shared__ float turned[32][kJoinColumns + 1];
   __shared__ float inv[32], ts[32];
   __shared__ int label[32], row[32];
   const int n = threadIdx.x & 31, g = threadIdx.x >> 5, i = row_tile * kOwned + wave * 32 + n;
   const int64_t item0 = (int64_t)row_tile * splits;
-  const float *stat = a.part_stat + (size_t)item0 * 3 * kOwned + wave * 32 + n;
   const int lab = a.label[i];
-  float m = kNoMax, others = 0.f, zl = -INFINITY;
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, stat[(size_t)s * 3 * kOwned]);
-  for (int s = 0; s < splits; ++s) {
-    const float *p = stat + (size_t)s * 3 * kOwned;
-    others += p[kOwned] * exp_diff(p[0], m);
-    if (lab >= 0 && (lab / kTile) / meta.tiles_per == s) zl = p[2 * kOwned];
+  float m = kNoMax;
+  for (int s = g; s < splits; s += 8) {
+    const float *p = a.part_stat + (size_t)(item0 + s) * 3 * kOwned + wave * 32 + n;
+    stat[0][s][n] = p[0];
+    stat[1][s][n] = p[kOwned];
+    stat[2][s][n] = p[2 * kOwned];
+    m = fmaxf(m, p[0]);
   }
-  const RowEnd e = end_row(m, others, zl);
+  red[g][n] = m;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) m = fmaxf(m, red[k][n]);
+  __syncthreads();
+  for (int s = g; s < splits; s += 8) {  // from maxima to factors
+    const float f = exp_diff(stat[0][s][n], m);
+    stat[0][s][n] = f;
+    stat[1][s][n] *= f;
+  }
+  __syncthreads();
   if (g == 0) {
+    float others = 0.f;
+    for (int s = 0; s < splits; ++s) others += stat[1][s][n];
+    const float zl = lab >= 0 ? stat[2][lab / kTile / meta.tiles_per][n] : -INFINITY;
+    const RowEnd e = end_row(m, others, zl);
     const bool on = i < meta.n;
     inv[n] = e.inv;
     ts[n] = e.t;
     label[n] = on ? lab : -1;
     row[n] = on ? a.list[i] : -1;
-    if (on) {
+    if (on && d0 == 0) {
       a.row_loss[a.list[i]] = e.loss;
       a.max[i] = m;
       a.log[i] = e.log;
@@ -667,17 +684,22 @@ __global__ __launch_bounds__(256) void head_join_kernel(const RowsArgs a) {
     }
   }
   if (!GRAD || a.dh == nullptr) return;
-  for (int d0 = 0; d0 < DP; d0 += 8) {
-    float x = 0.f;
-    for (int s = 0; s < splits; ++s)
-      x += a.part[(((size_t)(item0 + s) * 4 + wave) * DP + d0 + g) * 32 + n] * exp_diff(stat[(size_t)s * 3 * kOwned], m);
-    turned[n][d0 + g] = x;
+  const float *part = a.part + (((size_t)item0 * 4 + wave) * DP + d0 + g) * 32 + n;
+  float x = 0.f, y = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < splits; ++s) {
+    const float f = stat[0][s][n];
+    x = fmaf(part[(size_t)s * 4 * DP * 32], f, x);
+    y = fmaf(part[(size_t)s * 4 * DP * 32 + 8 * 32], f, y);
   }
+  turned[n][g] = x;
+  turned[n][g + 8] = y;
   __syncthreads();
-  for (int k = threadIdx.x; k < 32 * DP; k += 256) {
-    const int r = k / DP, c = k % DP;
-    if (label[r] >= 0 && c < a.d)
-      a.dh[(size_t)((int64_t)row[r] * a.ld_dh) + c] = (bf16_t)((turned[r][c] * inv[r] - ts[r] * (float)a.W[(size_t)label[r] * DP + c]) * a.inv_n);
+  for (int k = threadIdx.x; k < 32 * kJoinColumns; k += 256) {
+    const int r = k / kJoinColumns, c = k % kJoinColumns;
+    if (label[r] >= 0 && d0 + c < a.d)
+      a.dh[(size_t)((int64_t)row[r] * a.ld_dh) + d0 + c] =
+          (bf16_t)((turned[r][c] * inv[r] - ts[r] * (float)a.W[(size_t)label[r] * DP + d0 + c]) * a.inv_n);
   }
 }
 
@@ -922,32 +944,29 @@ __global__ __launch_bounds__(256) void head_list_kernel(const PrepareArgs a) {
     at += in_wave[0] + in_wave[1] + in_wave[2] + in_wave[3];
     __syncthreads();
   }
-  if ((int)blockIdx.x == a.n_counts - 1 && threadIdx.x == 0) {
+  if ((int)blockIdx.x == a.n_counts - 1 && wave == 0) {
     Meta m{};
     m.n = at;
     m.row_tiles = (at + kOwned - 1) / kOwned;
     // class ranges: as many as make the last round of workgroups a full one.  A range costs its tiles and about eight more (its
-    // rows, its partial sums and their reading).
-    const int tiles = (a.C + kTile - 1) / kTile;
-    int64_t best = -1;
-    for (int s = 1; s <= a.max_splits && m.row_tiles > 0; ++s) {
-      const int per = (tiles + s - 1) / s, real = (tiles + per - 1) / per;
-      const int64_t items = (int64_t)m.row_tiles * real, cost = (items + kRound - 1) / kRound * (per + (real > 1 ? 8 : 4));
-      if (real > 1 && items > kRowItems) break;
-      if (best < 0 || cost < best) {
-        best = cost;
-        m.splits = real;
-        m.tiles_per = per;
-      }
-    }
-    if (m.splits == 0) {
-      m.splits = 1;
-      m.tiles_per = tiles;
-    }
-    const int row_steps = (at + kTile - 1) / kTile, per = (row_steps + a.ranges - 1) / a.ranges;
-    m.rows_per = max(per, 1) * kTile;
-    m.ranges = (row_steps + max(per, 1) - 1) / max(per, 1);
-    *a.meta = m;
+    // rows, its partial sums and their reading).  Every lane weighs one number of ranges.
+    static_assert(kMaxSplits == 64, "a lane each");
+    const int tiles = (a.C + kTile - 1) / kTile, tried = lane + 1;
+    int per = (tiles + tried - 1) / tried;
+    const int real = (tiles + per - 1) / per;
+    const int64_t items = (int64_t)m.row_tiles * real;
+    const bool may = tried <= a.max_splits && (real == 1 || items <= kRowItems);
+    uint64_t cost = may ? (uint64_t)(((items + kRound - 1) / kRound * (per + (real > 1 ? 8 : 4))) << 6 | lane) : ~0ull;  // the fewest of equals
+    uint64_t least = cost;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) least = min(least, (uint64_t)__shfl_xor((unsigned long long)least, o));
+    m.splits = __shfl(real, (int)(least & 63));
+    m.tiles_per = __shfl(per, (int)(least & 63));
+    const int row_steps = (at + kTile - 1) / kTile;
+    per = max((row_steps + a.ranges - 1) / a.ranges, 1);
+    m.rows_per = per * kTile;
+    m.ranges = (row_steps + per - 1) / per;
+    if (lane == 0) *a.meta = m;
   }
 }
 
@@ -1016,7 +1035,7 @@ FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads) {
   p.n_counts = (int)std::max<int64_t>(1, (rows + kMetaBlock - 1) / kMetaBlock);
   p.pack_blocks = p.padded_rows * (p.DP / 8) / 256;
   // class ranges of eight tiles at least
-  p.max_splits = std::max(1, std::min(64, (C + 8 * kTile - 1) / (8 * kTile)));
+  p.max_splits = std::max(1, std::min(kMaxSplits, (C + 8 * kTile - 1) / (8 * kTile)));
   p.max_items = std::min(row_tiles * p.max_splits, std::max<int64_t>(row_tiles, kRowItems));
   // row ranges of the classes kernel: rounds of workgroups filled as far as the partial sums' room allows
   const int64_t steps = std::max<int64_t>(1, (rows + kTile - 1) / kTile);
@@ -1121,7 +1140,8 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   HEAD_TRY(hipGetLastError());
   if (p.max_splits > 1) {
     const unsigned blocks = 4u * (unsigned)std::min<int64_t>(p.padded_rows / kOwned, kRowItems);
-    hipLaunchKernelGGL((sums ? head_join_kernel<DP, true> : head_join_kernel<DP, false>), dim3(blocks), dim3(256), 0, s, r);
+    hipLaunchKernelGGL((sums ? head_join_kernel<DP, true> : head_join_kernel<DP, false>), dim3(blocks, sums ? (unsigned)((p.d + kJoinColumns - 1) / kJoinColumns) : 1u),
+                       dim3(256), 0, s, r);
     HEAD_TRY(hipGetLastError());
   }
   if (!c.dW && !c.db) return hipSuccess;

@@ -194,12 +194,13 @@ UpdateArgs adam_args(float lr, float b1, float b2, float eps, float wd, int64_t 
 
 struct Layout {
   size_t m = 0, v = 0, logits = 0, dlogits = 0, dtop = 0, row_loss = 0, scratch = 0, loss = 0, Wt = 0, Wn = 0, gemm_partial = 0,
-         bias_partial = 0, total = 0;
+         bias_partial = 0, head = 0, head_bytes = 0, total = 0;
 };
 
 struct Dims {
   int64_t n = 0, head_rows = 0, n_param_elems = 0;  // head_rows: of one block of the head's work
   int K = 0, d_top = 0, C = 0, Cp = 0, Kp = 0, dtype = 0, elt = 4;
+  bool fused = false;
 };
 
 bool read_dims(const gnntrain_desc *d, Dims &x, std::string &err) {
@@ -207,7 +208,11 @@ bool read_dims(const gnntrain_desc *d, Dims &x, std::string &err) {
   if (d->n_stages <= 0 || !d->stages) { err = "no stages"; return false; }
   for (int s = 0; s < d->n_stages; ++s)
     if (!d->stages[s]) { err = "a stage handle is NULL"; return false; }
-  if (d->n_classes <= 0 || d->n_classes > 65536) { err = "n_classes must be in [1, 65536]"; return false; }
+  x.fused = d->head_fused != 0;
+  if (d->n_classes <= 0 || d->n_classes > (x.fused ? 1 << 24 : 65536)) {
+    err = x.fused ? "n_classes must be in [1, 2^24]" : "n_classes must be in [1, 65536] (2^24 with head_fused)";
+    return false;
+  }
   if (d->n_params < 0 || (d->n_params > 0 && !d->params)) { err = "params is NULL"; return false; }
   if (d->optimizer != GNNTRAIN_SGD && d->optimizer != GNNTRAIN_ADAM) { err = "unknown optimizer"; return false; }
   if (d->alpha_hist < 1) { err = "alpha_hist must be at least 1"; return false; }
@@ -243,16 +248,23 @@ Layout make_layout(const gnntrain_desc *d, const Dims &x) {
   const size_t moments = d->optimizer == GNNTRAIN_ADAM ? sizeof(float) * (size_t)x.n_param_elems : 0;
   l.m = take(moments);
   l.v = take(moments);
-  l.logits = take(sizeof(float) * (size_t)x.head_rows * x.Cp);
-  l.dlogits = take((size_t)x.elt * x.n * x.Cp);
+  if (!x.fused) {
+    l.logits = take(sizeof(float) * (size_t)x.head_rows * x.Cp);
+    l.dlogits = take((size_t)x.elt * x.n * x.Cp);
+  }
   l.dtop = take((size_t)x.elt * x.n * x.d_top);
   l.row_loss = take(sizeof(float) * (size_t)x.n);
   l.scratch = take(sizeof(float) * 1024);
   l.loss = take(256);
-  l.Wt = take((size_t)x.elt * x.C * x.Kp);
-  l.Wn = take((size_t)x.elt * x.d_top * x.Cp);
-  l.gemm_partial = take(sizeof(float) * (size_t)kMaxSplits * x.d_top * x.C);
-  l.bias_partial = take(sizeof(float) * (size_t)kMaxSplits * x.Cp);
+  if (x.fused) {
+    l.head_bytes = gnntrain_head_xent_workspace_size(x.n, x.d_top, x.C, x.dtype, 1);
+    l.head = take(l.head_bytes);
+  } else {
+    l.Wt = take((size_t)x.elt * x.C * x.Kp);
+    l.Wn = take((size_t)x.elt * x.d_top * x.Cp);
+    l.gemm_partial = take(sizeof(float) * (size_t)kMaxSplits * x.d_top * x.C);
+    l.bias_partial = take(sizeof(float) * (size_t)kMaxSplits * x.Cp);
+  }
   l.total = off;
   return l;
 }
@@ -565,9 +577,11 @@ extern "C" int gnntrain_epoch(gnntrain_t *tr, int64_t epoch, float *loss, void *
   std::vector<FillArgs> grads;
   for (const gnntrain_param &p : tr->params) grads.push_back(FillArgs{p.grad, sizeof(float) * (size_t)p.count});
   TRAIN_HIP(tr, launch_fills_zero(grads.data(), (int)grads.size(), stream));
-  // the head's weights, staged like a layer's: transposed for the logits, plain for the input gradient
-  const StageWeightsArgs head{tr->head_W, x.d_top, x.C, tr->at<char>(lay.Wt), x.Kp, tr->at<char>(lay.Wn), x.Cp};
-  TRAIN_HIP(tr, launch_stage_weights(&head, 1, cd, nullptr, stream));
+  if (!x.fused) {
+    // the head's weights, staged like a layer's: transposed for the logits, plain for the input gradient
+    const StageWeightsArgs head{tr->head_W, x.d_top, x.C, tr->at<char>(lay.Wt), x.Kp, tr->at<char>(lay.Wn), x.Cp};
+    TRAIN_HIP(tr, launch_stage_weights(&head, 1, cd, nullptr, stream));
+  }
 
   char *dlogits = tr->at<char>(lay.dlogits);
   float *row_loss = tr->at<float>(lay.row_loss);
@@ -583,7 +597,13 @@ extern "C" int gnntrain_epoch(gnntrain_t *tr, int64_t epoch, float *loss, void *
     for (int pos = 0; pos < x.K; ++pos)
       for (int s = 0; s < S; ++s) TRAIN_STAGE(tr, s, stage_forward_chunk(tr->stages[(size_t)s], tr->order[(size_t)pos], pos, stream));
   }
-  for (int64_t row0 = 0; row0 < x.n; row0 += x.head_rows) {
+  if (x.fused) {
+    const int rc = gnntrain_head_xent(tr->top, x.d_top, tr->head_W, cd, tr->head_b, tr->labels, tr->mask, x.n, x.d_top, x.C, inv_n, row_loss,
+                                      tr->at<char>(lay.dtop), x.d_top, tr->head_dW, tr->head_db, tr->at<char>(lay.head), lay.head_bytes, stream);
+    if (rc != GNNSTAGE_OK) return fail(tr, rc, gnntrain_last_error(nullptr));
+  }
+  const int64_t head_n = x.fused ? 0 : x.n;  // rows of the head in blocks
+  for (int64_t row0 = 0; row0 < head_n; row0 += x.head_rows) {
     const int64_t M = std::min(x.head_rows, x.n - row0);
     GemmNtArgs g{};
     g.A = static_cast<const char *>(tr->top) + (size_t)row0 * x.d_top * x.elt;
@@ -605,7 +625,7 @@ extern "C" int gnntrain_epoch(gnntrain_t *tr, int64_t epoch, float *loss, void *
     if (rc != GNNSTAGE_OK) return fail(tr, rc, "softmax cross-entropy launch failed");
   }
   // ---- backward: the head, then the stages from the last to the first, each in reverse chunk order
-  for (int64_t row0 = 0; row0 < x.n; row0 += x.head_rows) {
+  for (int64_t row0 = 0; row0 < head_n; row0 += x.head_rows) {
     const int64_t M = std::min(x.head_rows, x.n - row0);
     const char *dl = dlogits + (size_t)row0 * x.Cp * x.elt;
     GemmTnArgs w{};

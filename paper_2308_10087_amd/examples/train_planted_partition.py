@@ -35,6 +35,8 @@ def main() -> None:
     ap.add_argument("--dropout", type=float, default=0.0,
                     help="inside ResGCN+ blocks and on the layer outputs of gcn / sage stages (not of the last stage, which feeds the head)")
     ap.add_argument("--bf16", action="store_true")
+    ap.add_argument("--head-fused", action="store_true", help="a loss head that keeps no logits")
+    ap.add_argument("--save-8bit", action="store_true", help="keep what the forward pass saves for the weight gradients in 8 bits")
     ap.add_argument("--partition", action="store_true",
                     help="chunks from the locality-aware partitioner (Algorithm 1's first step) instead of index ranges")
     ap.add_argument("--seed", type=int, default=1)
@@ -88,7 +90,7 @@ def main() -> None:
         st = g.GnnStage(row_ptr, col, chunk_ptr, dims, W=W, cur=cur, hist=hist, dW=dW, bias=bias, dbias=dbias, variant=variant[kind],
                         dtype=g.GNNSTAGE_BF16 if args.bf16 else g.GNNSTAGE_F32, level0_f32=(l0 == torch.float32 and args.bf16),
                         grad_in=grad_in, device=dev, ln_gamma=ln[0], ln_beta=ln[1], d_ln_gamma=ln[2], d_ln_beta=ln[3],
-                        dropout_p=args.dropout if (kind == "resgcn" or si < len(kinds) - 1) else 0.0)
+                        save_8bit=args.save_8bit, dropout_p=args.dropout if (kind == "resgcn" or si < len(kinds) - 1) else 0.0)
         stages.append(st)
         params += [(master[j], W[j] if args.bf16 else None, dW[j]) for j in range(2)]
         params += [(bias[j], None, dbias[j]) for j in range(2)]
@@ -106,7 +108,7 @@ def main() -> None:
     mask = torch.from_numpy(train_mask).to(dev)
     trainer = g.GnnTrainer(stages, head_W=head_W, head_b=head_b, head_dW=head_dW, head_db=head_db, labels=labels, train_mask=mask,
                            params=params, optimizer=g.GNNTRAIN_ADAM, lr=args.lr, shuffle=True, seed=args.seed,
-                           alpha_hist=args.alpha_hist, device=dev)
+                           alpha_hist=args.alpha_hist, head_fused=args.head_fused, device=dev)
     held_out = torch.from_numpy(train_mask == 0).to(dev)
     for epoch in range(args.epochs):
         loss = trainer.gnntrain_epoch(epoch)
