@@ -138,8 +138,8 @@ typedef struct {
   float dropout_p; /* in [0, 1), 0 = none.  GNNSTAGE_RESGCN: between ReLU and the convolution; GNNSTAGE_GCN,
                       GNNSTAGE_SAGE: on every layer's output; GNNSTAGE_GCNII: must be 0 */
   int32_t save_8bit; /* non-zero: what the forward pass saves for the weight gradients (the aggregations of layers that aggregate
-                        first, gnnstage_layer_order) is kept in 8 bits, see gnnstage_rows8_store.  Levels, gradients of rows and bias gradients are
-                        the same bits as without; weight gradients are those of the stored values */
+                        first, gnnstage_layer_order) is kept in 8 bits, see gnnstage_rows8_store.  Levels and gradients of rows are the same bits
+                        as without, bias gradients the same sums (bf16: in another order); weight gradients are those of the stored values */
 } gnnstage_desc;
 
 /* Device bytes the stage needs inside desc->workspace (graph tables, transposed index,

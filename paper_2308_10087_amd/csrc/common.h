@@ -384,7 +384,7 @@ struct GemmTnArgs {
   float *bias_partial;  // fp32 scratch [splits][O]
   const uint8_t *a_scale = nullptr;  // a_dtype DT_ROWS8: the factors of A's rows, a byte per 32 columns
   int32_t ld_scale = 0;
-  int32_t b_cols = 0;             // columns of B that may be read (0: ldb)
+  int32_t b_cols = 0;             // a_dtype DT_ROWS8: columns of B that may be read (0: ldb)
   int32_t wide_min_rows = 65536;  // bf16 operands from this many rows on, with more than one 128 x 128 output tile: one
                                   // workgroup per row split computes the whole output (tests force it on small inputs)
 };

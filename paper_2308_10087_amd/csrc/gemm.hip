@@ -14,6 +14,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "lds_tile.h"
 
 namespace {
 
@@ -199,18 +200,6 @@ __device__ inline bf16x8 load8_bf16(const T *base, size_t ld, int r, int c, int 
 #pragma unroll
     for (int t = 0; t < 8; ++t)
       if (c + t < cols) out[t] = (bf16_t)to_f32(p[t]);
-  }
-  return out;
-}
-
-// 8 consecutive columns (from a multiple of 8 on) of a row kept in 8 bits, exactly as bf16; columns >= cols read as zero
-__device__ inline bf16x8 load8_rows8(const int8_t *q, size_t ld, const uint8_t *scale, size_t ld_scale, int r, int c, int cols) {
-  bf16x8 out = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (c < cols) {
-    const u32x2 w = *reinterpret_cast<const u32x2 *>(q + (size_t)r * ld + c);
-    const float f = __builtin_bit_cast(float, (uint32_t)scale[(size_t)r * ld_scale + (c >> 5)] << 23);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) out[t] = (bf16_t)((float)(int8_t)(w[t >> 2] >> (8 * (t & 3))) * f);
   }
   return out;
 }
@@ -683,8 +672,7 @@ __global__ __launch_bounds__(256) void gemm_tn_bf16_kernel(const Batch<GemmTnWor
   const TA *A = static_cast<const TA *>(a.A);
   const bf16_t *B = static_cast<const bf16_t *>(a.B);
   const bf16x8 zero8 = {0, 0, 0, 0, 0, 0, 0, 0};
-  constexpr bool ROWS8 = std::is_same<TA, int8_t>::value;
-  const int a_cols = ROWS8 ? (a.I + 31) / 32 * 32 : VEC ? a.lda : a.I;
+  const int a_cols = VEC ? a.lda : a.I;
 
   f32x16 acc[2][2];
 #pragma unroll
@@ -727,11 +715,8 @@ __global__ __launch_bounds__(256) void gemm_tn_bf16_kernel(const Batch<GemmTnWor
     for (int i = 0; i < NVT; ++i) {
       const int r = 2 * ((tid >> 4) + 16 * (i >> 1)) + (i & 1), c = (tid & 15) * 8;  // slots 2h, 2h+1: one row pair
       const bool rv = r0 + r < r_end;
-      if constexpr (ROWS8)
-        ra[i] = rv ? load8_rows8(A, (size_t)a.lda, a.a_scale, (size_t)a.ld_scale, r0 + r, i0 + c, a_cols) : zero8;
-      else if constexpr (!PAIR)
-        ra[i] = rv ? load8_bf16<TA, VEC>(A, (size_t)a.lda, r0 + r, i0 + c, a_cols) : zero8;
-      rb[i] = (rv && o0 + c < a.b_cols) ? *reinterpret_cast<const bf16x8 *>(B + (size_t)(r0 + r) * a.ldb + o0 + c) : zero8;
+      if constexpr (!PAIR) ra[i] = rv ? load8_bf16<TA, VEC>(A, (size_t)a.lda, r0 + r, i0 + c, a_cols) : zero8;
+      rb[i] = (rv && o0 + c < a.ldb) ? *reinterpret_cast<const bf16x8 *>(B + (size_t)(r0 + r) * a.ldb + o0 + c) : zero8;
     }
   };
   if (r_begin < r_end) gload(r_begin);
@@ -809,8 +794,6 @@ __global__ __launch_bounds__(256) void gemm_tn_bf16_kernel(const Batch<GemmTnWor
 // only in part through their XCD's L2 (measured on 10 M rows: 16.1 GB fetched for 10.2 GB of operands).  A wave owns
 // 64 rows x 128 columns of the output (eight 32 x 32 accumulators); both operands are bf16 with 16-byte aligned rows.
 constexpr int LDS_PW = 260;  // padded stride, in words, of one row pair of a 256-column LDS tile
-// TA: bf16_t, or int8_t for A rows kept in 8 bits
-template <typename TA>
 __global__ __launch_bounds__(512) void gemm_tn_bf16_wide_kernel(const Batch<GemmTnWork> ba) {
   const GemmTnWork &work_of = ba.sub[blockIdx.z];
   const GemmTnArgs a = work_of.a;
@@ -823,7 +806,7 @@ __global__ __launch_bounds__(512) void gemm_tn_bf16_wide_kernel(const Batch<Gemm
   const int wi = (wave >> 1) * 64, wo = (wave & 1) * 128;
   const int r_begin = split * rows_per_split;
   const int r_end = min(a.M, r_begin + rows_per_split);
-  const TA *A = static_cast<const TA *>(a.A);
+  const bf16_t *A = static_cast<const bf16_t *>(a.A);
   const bf16_t *B = static_cast<const bf16_t *>(a.B);
   const bf16x8 zero8 = {0, 0, 0, 0, 0, 0, 0, 0};
 
@@ -849,11 +832,8 @@ __global__ __launch_bounds__(512) void gemm_tn_bf16_wide_kernel(const Batch<Gemm
     for (int i = 0; i < NVT; ++i) {
       const int r = 2 * ((tid >> 5) + 16 * (i >> 1)) + (i & 1);  // slots 2h, 2h+1: one row pair
       const bool rv = r0 + r < r_end;
-      if constexpr (std::is_same<TA, int8_t>::value)
-        ra[i] = rv ? load8_rows8(A, (size_t)a.lda, a.a_scale, (size_t)a.ld_scale, r0 + r, c, (a.I + 31) / 32 * 32) : zero8;
-      else
-        ra[i] = (rv && c < a.lda) ? *reinterpret_cast<const bf16x8 *>(A + (size_t)(r0 + r) * a.lda + c) : zero8;
-      rb[i] = (rv && c < a.b_cols) ? *reinterpret_cast<const bf16x8 *>(B + (size_t)(r0 + r) * a.ldb + c) : zero8;
+      ra[i] = (rv && c < a.lda) ? *reinterpret_cast<const bf16x8 *>(A + (size_t)(r0 + r) * a.lda + c) : zero8;
+      rb[i] = (rv && c < a.ldb) ? *reinterpret_cast<const bf16x8 *>(B + (size_t)(r0 + r) * a.ldb + c) : zero8;
     }
   };
   if (r_begin < r_end) gload(r_begin);
@@ -921,6 +901,162 @@ __global__ __launch_bounds__(512) void gemm_tn_bf16_wide_kernel(const Batch<Gemm
       for (int t = 0; t < 16; ++t) {
         const int ii = wi + i * 32 + 8 * (t >> 2) + 4 * (lane >> 5) + (t & 3);
         const int oo = wo + j * 32 + (lane & 31);
+        if (ii < a.I && oo < a.O) P[(size_t)ii * a.O + oo] = acc[i][j][t];
+      }
+}
+
+// The product of rows kept in 8 bits (A, see rows8.hip) with bf16 rows.  One workgroup of eight waves owns a row split and 128 IT x 64 OT
+// outputs (256 x 256: all of a usual layer's, so that every row is read once), a wave 32 IT x 32 OT of them.  Bound by memory,
+// (33 / 32 I + 2 O) bytes a row.  32 rows at a time go through registers, where A becomes bf16 (exactly: whole numbers of 7 bits
+// times powers of two) and B's columns are added up, into one of two LDS buffers, and are multiplied from there by transpose reads; the
+// loads of two more tiles are under way meanwhile (50 KB per compute unit at 256 x 256).  The workgroups take tiles in turn, so that what the chip
+// reads at a time lies side by side.
+// 700 k rows, 256 x 256: 408 us with row pairs packed by the vector ALU (as in the kernels above), 220 us with direct-to-LDS loads, whose
+// tiles cost two more passes through LDS.
+template <int IT, int OT>
+__global__ __launch_bounds__(512) void gemm_tn_rows8_kernel(const Batch<GemmTnWork> ba) {
+  constexpr int I = 128 * IT, O = 64 * OT, R = 32;
+  constexpr int PER = R * I / 512;            // A: values of a thread, 8 or 16 side by side
+  constexpr int PIECES = O / 8, ROWS = 512 / PIECES, PASSES = ROWS < R ? R / ROWS : 1;  // B: pieces of a row; rows of a pass of the workgroup
+  const GemmTnWork &work_of = ba.sub[blockIdx.z];
+  const GemmTnArgs &a = work_of.a;
+  const int splits = work_of.splits;
+  __shared__ __attribute__((aligned(1024))) char A0[R * I * 2], A1[R * I * 2], B0[R * O * 2], B1[R * O * 2];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int ti = (a.I + I - 1) / I, tiles = ti * ((a.O + O - 1) / O);
+  const int tile = blockIdx.x % tiles, split = blockIdx.x / tiles;
+  if (split >= splits) return;
+  const int i0 = (tile % ti) * I, o0 = (tile / ti) * O;
+  const int wi = (wave >> 1) * IT, wo = (wave & 1) * OT;  // this wave's first output tiles
+  const int M = a.M, steps = ((M + R - 1) / R - split + splits - 1) / splits;
+  const int lda = a.lda, ldb = a.ldb, lds = a.ld_scale;
+  const int a_cols = (a.I + 31) / 32 * 32 - i0, b_cols = a.b_cols - o0;
+  const int ar = tid * PER / I, ac = tid * PER % I, br = tid / PIECES, bc = tid % PIECES * 8;
+  const bool a_in = ac < a_cols, b_in = bc < b_cols;
+  const int8_t *const Ab = static_cast<const int8_t *>(a.A) + i0 + (a_in ? ac : 0);
+  const uint8_t *const Sb = a.a_scale + ((i0 + (a_in ? ac : 0)) >> 5);
+  const bf16_t *const Bb = static_cast<const bf16_t *>(a.B) + o0 + (b_in ? bc : 0);
+  struct Regs {
+    uint32_t q[PER / 4], s;
+    bf16x8 b[PASSES];
+  } x0, x1;
+  // Every lane loads, past the end what is there last: no branch, so that the compiler knows which loads are out.
+  auto load = [&](int t, Regs &x) {
+    const int64_t r0 = ((int64_t)min(t, steps - 1) * splits + split) * R;
+    const int last = (int)min((int64_t)R, M - r0) - 1;
+    const int8_t *const Ar = Ab + r0 * lda;
+    const uint8_t *const Sr = Sb + r0 * lds;
+    const bf16_t *const Br = Bb + r0 * ldb;
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) x.b[k] = *reinterpret_cast<const bf16x8 *>(Br + min(br + k * ROWS, last) * ldb);
+    if constexpr (PER == 16) {
+      const u32x4 w = *reinterpret_cast<const u32x4 *>(Ar + min(ar, last) * lda);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x.q[k] = w[k];
+    } else {
+      const u32x2 w = *reinterpret_cast<const u32x2 *>(Ar + min(ar, last) * lda);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) x.q[k] = w[k];
+    }
+    x.s = Sr[min(ar, last) * lds];
+  };
+  const bool do_bias = a.bias_partial != nullptr && i0 == 0;
+  float bsum[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) bsum[t] = 0.f;
+  auto write = [&](int t, const Regs &x, char *as, char *bs) {
+    const int64_t r0 = ((int64_t)t * splits + split) * R;
+    const int left = t < steps ? (int)min((int64_t)R, M - r0) : 0;
+    const float f = a_in && ar < left ? __builtin_bit_cast(float, x.s << 23) : 0.f;
+#pragma unroll
+    for (int k = 0; k < PER / 8; ++k) {
+      bf16x8 v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = (bf16_t)((float)(int8_t)(x.q[2 * k + (e >> 2)] >> (8 * (e & 3))) * f);
+      *reinterpret_cast<bf16x8 *>(as + lds_piece<I>(ar, ac / 8 + k)) = v;
+    }
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k) {
+      const int r = br + k * ROWS;
+      bf16x8 v = x.b[k];
+      if (!b_in || r >= left) v = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (ROWS <= R || r < R) *reinterpret_cast<bf16x8 *>(bs + lds_piece<O>(r, bc / 8)) = v;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bsum[e] += (float)v[e];
+    }
+  };
+  f32x16 acc[IT][OT];
+#pragma unroll
+  for (int i = 0; i < IT; ++i)
+#pragma unroll
+    for (int j = 0; j < OT; ++j)
+#pragma unroll
+      for (int t = 0; t < 16; ++t) acc[i][j][t] = 0.f;
+  uint32_t place_a = lds_turn_place<I>(lane), place_b = lds_turn_place<O>(lane);
+  auto multiply = [&](const char *as, const char *bs) {
+    asm volatile("" : "+v"(place_a), "+v"(place_b));
+#pragma unroll
+    for (int k = 0; k < R / 16; ++k) {
+      bf16x8 fa[IT];
+#pragma unroll
+      for (int i = 0; i < IT; ++i) fa[i] = lds_turned_at<I>((const lds_char *)as, place_a, wi + i, k);
+#pragma unroll
+      for (int j = 0; j < OT; ++j) {
+        const bf16x8 fb = lds_turned_at<O>((const lds_char *)bs, place_b, wo + j, k);
+#pragma unroll
+        for (int i = 0; i < IT; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb, acc[i][j], 0, 0, 0);
+      }
+    }
+  };
+  // One barrier a tile: a tile is multiplied while the next one is written to the other buffer, and the two behind it are loaded.
+  auto step = [&](int t, const char *as, const char *bs, Regs &next, char *next_as, char *next_bs) {
+    lds_barrier();
+    write(t + 1, next, next_as, next_bs);
+    load(t + 3, next);
+    multiply(as, bs);
+  };
+  // (in this order: what the loop waits for is counted from the newest load on)
+  load(0, x0);
+  __builtin_amdgcn_sched_barrier(0);
+  load(1, x1);
+  __builtin_amdgcn_sched_barrier(0);
+  write(0, x0, A0, B0);
+  load(2, x0);
+  __builtin_amdgcn_sched_barrier(0);
+  for (int t = 0; t < steps; t += 2) {
+    step(t, A0, B0, x1, A1, B1);
+    if (t + 1 < steps) step(t + 1, A1, B1, x0, A0, B0);
+  }
+  if (do_bias) {  // the threads' column sums, in B's buffers
+    lds_barrier();
+    constexpr int HALF = R * O * 2 / 32;  // threads whose eight sums fit one buffer
+    constexpr int GROUPS = ROWS < R ? ROWS : R, ADDERS = GROUPS * PIECES;
+    static_assert(2 * HALF >= ADDERS, "room for all threads' sums");
+    float *const c0 = reinterpret_cast<float *>(B0), *const c1 = reinterpret_cast<float *>(B1);
+    if (tid < ADDERS) {
+      float *mine = tid < HALF ? c0 + tid * 8 : c1 + (tid - HALF) * 8;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) mine[t] = bsum[t];
+    }
+    __syncthreads();
+    if (tid < O && o0 + tid < a.O) {  // column tid: the threads g * PIECES + tid / 8, element tid % 8
+      float sum = 0.f;
+      for (int g = 0; g < GROUPS; ++g) {
+        const int from = g * PIECES + (tid >> 3);
+        sum += (from < HALF ? c0 + from * 8 : c1 + (from - HALF) * 8)[tid & 7];
+      }
+      a.bias_partial[(size_t)split * a.O + o0 + tid] = sum;
+    }
+  }
+  float *P = a.partial + (size_t)split * a.I * a.O;
+#pragma unroll
+  for (int i = 0; i < IT; ++i)
+#pragma unroll
+    for (int j = 0; j < OT; ++j)
+#pragma unroll
+      for (int t = 0; t < 16; ++t) {
+        const int ii = i0 + (wi + i) * 32 + 8 * (t >> 2) + 4 * (lane >> 5) + (t & 3);
+        const int oo = o0 + (wo + j) * 32 + (lane & 31);
         if (ii < a.I && oo < a.O) P[(size_t)ii * a.O + oo] = acc[i][j][t];
       }
 }
@@ -1503,10 +1639,29 @@ struct TnPlan {
   unsigned gx, threads;
   size_t count() const { return (size_t)w.a.I * w.a.O; }
 };
+// Rows kept in 8 bits with bf16 ones: outputs and splits.
+static int plan_rows8(const GemmTnArgs &a, TnPlan &p) {
+  if (!vec_ok(a.B, a.ldb, 8) || !aligned16(a.A) || a.lda % 16 != 0 || std::max(a.lda, std::max(a.ldb, a.ld_scale)) >= 1 << 24) return hipErrorInvalidValue;  // (offsets of a tile's rows in 32 bits)
+  const int it = a.I <= 128 ? 1 : 2, ot = a.O <= 64 ? 1 : a.O <= 128 ? 2 : 4;
+  const int tiles = (a.I + 128 * it - 1) / (128 * it) * ((a.O + 64 * ot - 1) / (64 * ot));
+  // a workgroup per compute unit (two where two fit), as long as each has four tiles of rows to read ahead in
+  int splits = std::min((it * ot >= 4 ? 256 : 512) / tiles, (a.M + 127) / 128);
+  splits = std::max(1, std::min(splits, a.max_splits));
+  const int rows_per = ((a.M + splits - 1) / splits + 31) / 32 * 32;
+  splits = (a.M + rows_per - 1) / rows_per;
+  p.w = GemmTnWork{a, rows_per, splits};
+  p.threads = 512;
+  p.gx = (unsigned)(splits * tiles);
+  static const tn_fn table[2][3] = {{gemm_tn_rows8_kernel<1, 1>, gemm_tn_rows8_kernel<1, 2>, gemm_tn_rows8_kernel<1, 4>},
+                                    {gemm_tn_rows8_kernel<2, 1>, gemm_tn_rows8_kernel<2, 2>, gemm_tn_rows8_kernel<2, 4>}};
+  p.fn = table[it - 1][ot == 4 ? 2 : ot - 1];
+  return hipSuccess;
+}
 static int plan_gemm_tn(const GemmTnArgs &a_in, int compute_dtype, TnPlan &p) {
   GemmTnArgs a = a_in;
   const bool rows8 = a.a_dtype == DT_ROWS8;
   if (a.b_cols == 0) a.b_cols = a.ldb;
+  if (rows8 && compute_dtype == DT_BF16) return plan_rows8(a, p);
   const bool narrow = (a.I < 4 && !rows8) || a.O < 4;  // fp32 operands of fewer columns than a 16-byte vector
   const int tile = compute_dtype == DT_BF16 ? 128 : narrow ? 16 : 64;
   const int step = compute_dtype == DT_BF16 ? TR : 16;
@@ -1524,8 +1679,8 @@ static int plan_gemm_tn(const GemmTnArgs &a_in, int compute_dtype, TnPlan &p) {
   if (splits < 1) splits = 1;
   if (splits > a.max_splits) splits = a.max_splits;
   // long operands with more than one 128 x 128 output tile: one workgroup per row split computes all of the output
-  const bool wide = compute_dtype == DT_BF16 && (a.a_dtype == DT_BF16 || rows8) && a.M >= a.wide_min_rows && ti * to > 1 && a.I <= 256 &&
-                    a.O <= 256 && (rows8 || vec_ok(a.A, a.lda, 8)) && vec_ok(a.B, a.ldb, 8);
+  const bool wide = compute_dtype == DT_BF16 && a.a_dtype == DT_BF16 && a.M >= a.wide_min_rows && ti * to > 1 && a.I <= 256 &&
+                    a.O <= 256 && vec_ok(a.A, a.lda, 8) && vec_ok(a.B, a.ldb, 8);
   if (wide) splits = a.max_splits < 256 ? a.max_splits : 256;  // one workgroup per compute unit
   int rows_per = (a.M + splits - 1) / splits;
   rows_per = (rows_per + step - 1) / step * step;
@@ -1533,11 +1688,11 @@ static int plan_gemm_tn(const GemmTnArgs &a_in, int compute_dtype, TnPlan &p) {
   p.w = GemmTnWork{a, rows_per, splits};
   p.threads = wide ? 512 : 256;
   if (wide) {
-    p.fn = rows8 ? gemm_tn_bf16_wide_kernel<int8_t> : gemm_tn_bf16_wide_kernel<bf16_t>;
+    p.fn = gemm_tn_bf16_wide_kernel;
     p.gx = (unsigned)splits;
   } else if (compute_dtype == DT_BF16) {
     p.gx = (unsigned)(((splits + 7) / 8) * 8 * ti * to);
-    p.fn = rows8 ? gemm_tn_bf16_kernel<int8_t, true> : a.a_dtype == DT_F32 ? (pair_ok(a.A, a.lda) ? gemm_tn_bf16_kernel<float, false, true> : gemm_tn_bf16_kernel<float, false>)
+    p.fn = a.a_dtype == DT_F32 ? (pair_ok(a.A, a.lda) ? gemm_tn_bf16_kernel<float, false, true> : gemm_tn_bf16_kernel<float, false>)
                                : (vec_ok(a.A, a.lda, 8) ? gemm_tn_bf16_kernel<bf16_t, true> : gemm_tn_bf16_kernel<bf16_t, false>);
   } else {
     if (a.a_dtype != DT_F32 && !rows8) return hipErrorInvalidValue;

@@ -16,6 +16,7 @@
 
 #include "../../include/gnntrain.h"
 #include "common.h"
+#include "lds_tile.h"
 
 namespace {
 
@@ -351,9 +352,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef bf16_t bf16x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-#define LDS_AS __attribute__((address_space(3)))
-typedef LDS_AS char lds_char;
 
 constexpr float kLog2e = 1.44269504088896f;
 constexpr float kNoMax = -3.4028234663852886e38f;  // the least number: of a row that has seen no more than minus infinity
@@ -376,20 +374,11 @@ struct Meta {
   int32_t unused[2];
 };
 
-// 16-byte pieces of an LDS tile row are permuted by the row, so that neither the row-wise reads of the first product (32 rows, one
-// column piece) nor the transpose reads of the second (four rows, 64 bytes) meet in a bank: no conflicts counted at width 256.
-template <int DP>
-__host__ __device__ constexpr int swizzle(int row) {
-  return DP >= 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
-}
 template <int DP>
 struct Geometry {
   static constexpr int row_bytes = DP * 2, chunks = DP / 8, rows_per_load = 64 / chunks, loads = kTile / (4 * rows_per_load);
   static constexpr int tile_bytes = kTile * row_bytes;
 };
-__device__ __forceinline__ void load_lds16(const void *g, lds_char *l) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g, (LDS_AS void *)l, 16, 0, 0);
-}
 // A lane's places in a tile: of what it loads, of its rows in the first product, of its columns in the second.
 template <int DP>
 struct Places {
@@ -397,11 +386,9 @@ struct Places {
   __device__ Places(int wave, int lane) {
     typedef Geometry<DP> G;
     const int row = wave * G::rows_per_load + lane / G::chunks;
-    load = row * G::row_bytes + (((lane % G::chunks) ^ swizzle<DP>(row)) << 4);
-    const int r = lane & 31, h = lane >> 5;
-    first = r * G::row_bytes + ((h ^ swizzle<DP>(r)) << 4);
-    const int in_half = (lane >> 4) & 1, t = (lane & 15) >> 2, u = lane & 3;  // transpose read: row t, 4 columns from 16 in_half + 4 u
-    second = (4 * h + t) * G::row_bytes + (((2 * in_half + (u >> 1)) ^ swizzle<DP>(4 * h + t)) << 4) + (u & 1) * 8;
+    load = lds_piece<DP>(row, lane % G::chunks);
+    first = lds_piece<DP>(lane & 31, lane >> 5);
+    second = lds_turn_place<DP>(lane);
   }
   // the addresses below are these with constant bits turned over; made anew in every step, or the compiler keeps them all in
   // registers and spills
@@ -414,23 +401,13 @@ __device__ __forceinline__ void load_tile(const bf16_t *src, lds_char *dst, int 
   for (int q = 0; q < G::loads; ++q) {
     constexpr int step = 4 * G::rows_per_load;
     // (the q-th load's row is step rows on: its swizzle differs where step / 4 is odd)
-    const uint32_t turn = (swizzle<DP>(q * step) ^ swizzle<DP>(0)) << 4;
+    const uint32_t turn = (lds_swizzle<DP>(q * step) ^ lds_swizzle<DP>(0)) << 4;
     load_lds16(reinterpret_cast<const char *>(src) + (place ^ turn) + q * step * G::row_bytes, dst + q * step * G::row_bytes + wave * 1024);
   }
 }
 template <int DP>
 __device__ __forceinline__ bf16x8 first_operand(const lds_char *tile, uint32_t place, int ks) {
   return *reinterpret_cast<const LDS_AS bf16x8 *>(tile + (place ^ ((32 * ks) & (Geometry<DP>::row_bytes - 1) & 255)) + ((32 * ks) & ~255));
-}
-template <int DP>
-__device__ __forceinline__ bf16x8 second_operand(const lds_char *tile, uint32_t place, int dt, int t) {
-  typedef Geometry<DP> G;
-  const uint32_t at = (place ^ ((dt & 3) * 64)) + (dt >> 2) * 256 + 16 * t * G::row_bytes;
-  // (the second half is 8 rows on: swizzle turned over in its second bit)
-  const uint32_t at2 = (place ^ ((dt & 3) * 64 + 32)) + (dt >> 2) * 256 + (16 * t + 8) * G::row_bytes;
-  const bf16x4 x = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + at)));
-  const bf16x4 y = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4 *)(tile + at2)));
-  return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 // The owned vectors as right operands of the first product: most in registers; the rest, where the registers do not reach, in LDS.
 template <int DP, int IN_REGS>
@@ -572,7 +549,7 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(const RowsArgs a) {
       for (int dt = 0; dt < DP / 32; ++dt)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-          sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(second_operand<DP>(now, at.second, dt, t), p[t], sum[dt], 0, 0, 0);
+          sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_turned<DP>(now, at.second, dt, t), p[t], sum[dt], 0, 0, 0);
     }
   };
   if (begin < end) load(begin, (lds_char *)tile0, bias0);
@@ -794,7 +771,7 @@ __global__ __launch_bounds__(256, 2) void head_classes_kernel(const ClassesArgs 
     for (int dt = 0; dt < DP / 32; ++dt)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const bf16x8 x = second_operand<DP>(now, at.second, dt, t);
+        const bf16x8 x = lds_turned<DP>(now, at.second, dt, t);
         sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, high[t], sum[dt], 0, 0, 0);
         sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, low[t], sum[dt], 0, 0, 0);
       }

@@ -235,8 +235,8 @@ extern "C" int gnnstage_rows8_weight_grad(const int8_t *q, int64_t ld_q, const u
   std::string err;
   if (dtype != GNNSTAGE_F32 && dtype != GNNSTAGE_BF16) return stage_error(GNNSTAGE_EINVAL, std::string(me) + "unknown dtype");
   if (!sizes_ok(rows, d, err) || !sizes_ok(rows, d_out, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
-  if (ld_dy < d_out || ld_dy > INT32_MAX || ld_q > INT32_MAX || ld_s > INT32_MAX)
-    return stage_error(GNNSTAGE_EINVAL, std::string(me) + "a leading dimension is below the width or beyond 2^31 - 1");
+  if (ld_dy < d_out || ld_dy > INT32_MAX || ld_q >= 1 << 24 || ld_s >= 1 << 24)
+    return stage_error(GNNSTAGE_EINVAL, std::string(me) + "ld_dy is below d_out or beyond 2^31 - 1, or ld_q or ld_s beyond 2^24 - 1");
   if (rows == 0) return GNNSTAGE_OK;
   if (!dY || !dW) return stage_error(GNNSTAGE_EINVAL, std::string(me) + "dY and dW must not be NULL");
   if (!stored_ok(q, ld_q, scale, ld_s, d, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
@@ -246,7 +246,7 @@ extern "C" int gnnstage_rows8_weight_grad(const int8_t *q, int64_t ld_q, const u
     return stage_error(GNNSTAGE_ENOMEM, std::string(me) + "workspace smaller than gnnstage_rows8_weight_grad_workspace_size()");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   char *ws = static_cast<char *>(workspace);
-  const bool copy = dtype == GNNSTAGE_BF16 && ((reinterpret_cast<uintptr_t>(dY) & 15u) || ld_dy % 8 != 0 || d_out % 8 != 0);
+  const bool copy = dtype == GNNSTAGE_BF16 && ((reinterpret_cast<uintptr_t>(dY) & 15u) || ld_dy % 8 != 0 || d_out % 8 != 0 || ld_dy >= 1 << 24);
   const int64_t step = copy ? l.dy_rows : kMostRows;
   const int elt = dtype == GNNSTAGE_BF16 ? 2 : 4;
   for (int64_t r = 0; r < rows; r += step) {
