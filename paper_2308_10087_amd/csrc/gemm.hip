@@ -1023,10 +1023,12 @@ __global__ __launch_bounds__(512) void gemm_tn_rows8_kernel(const Batch<GemmTnWo
   write(0, x0, A0, B0);
   load(2, x0);
   __builtin_amdgcn_sched_barrier(0);
-  for (int t = 0; t < steps; t += 2) {
+  int t = 0;
+  for (; t + 2 <= steps; t += 2) {
     step(t, A0, B0, x1, A1, B1);
-    if (t + 1 < steps) step(t + 1, A1, B1, x0, A0, B0);
+    step(t + 1, A1, B1, x0, A0, B0);
   }
+  if (t < steps) step(t, A0, B0, x1, A1, B1);
   if (do_bias) {  // the threads' column sums, in B's buffers
     lds_barrier();
     constexpr int HALF = R * O * 2 / 32;  // threads whose eight sums fit one buffer
