@@ -359,7 +359,10 @@ constexpr float kNoMax = -3.4028234663852886e38f;  // the least number: of a row
 __device__ __forceinline__ float exp_diff(float z, float m) { return __builtin_amdgcn_exp2f((z - m) * kLog2e); }
 constexpr int kTile = 32;           // streamed vectors of a step
 constexpr int kOwned = 128;         // owned vectors of a workgroup, 32 per wave
-constexpr int kRound = 512;         // workgroups that run at once, two per compute unit
+// Workgroups that run at once: per compute unit two (width 256: a wave's sums are half of the registers), three or four.
+template <int DP>
+constexpr int kPerUnit = DP == 256 ? 2 : DP == 128 ? 3 : 4;
+int round_of(int DP) { return 256 * (DP == 256 ? kPerUnit<256> : DP == 128 ? kPerUnit<128> : kPerUnit<64>); }
 constexpr int kRowItems = 1536;     // most (row tile, class range) pairs that leave partial sums
 constexpr int kMetaBlock = 2048;    // rows of a counting workgroup
 
@@ -369,8 +372,8 @@ struct Meta {
   int32_t row_tiles;       // of kOwned
   int32_t splits;          // class ranges of the rows kernel
   int32_t tiles_per;       // class tiles of a range
-  int32_t rows_per;        // rows of a row range of the classes kernel (a multiple of kTile)
-  int32_t ranges;          // row ranges
+  int32_t row_steps;       // tiles of kTile rows: what a class tile of the classes kernel streams
+  int32_t groups;          // workgroups of the classes kernel that have work
   int32_t unused[2];
 };
 
@@ -415,9 +418,10 @@ struct Owned {
   static constexpr int steps = DP / 16, in_lds = steps - IN_REGS;
   bf16x8 reg[IN_REGS];
   lds_char *lds;
-  __device__ __forceinline__ Owned(const bf16_t *vectors, int64_t first, int wave, int lane, char *shared) {
+  // vector: this lane's (lane % 32 of the wave's 32)
+  __device__ __forceinline__ Owned(const bf16_t *vector, int wave, int lane, char *shared) {
     lds = (lds_char *)shared + wave * in_lds * 1024 + lane * 16;
-    const bf16_t *v = vectors + (size_t)(first + (lane & 31)) * DP + 8 * (lane >> 5);
+    const bf16_t *v = vector + 8 * (lane >> 5);
 #pragma unroll
     for (int i = 0; i < steps; ++i) {
       const bf16x8 x = *reinterpret_cast<const bf16x8 *>(v + 16 * i);
@@ -445,19 +449,44 @@ __device__ __forceinline__ void wait_tile() {
 
 struct RowsArgs {
   const Meta *meta;
-  const bf16_t *rows, *W;   // packed [.][DP]
+  const bf16_t *rows, *W;   // DIRECT: the caller's rows, which the list picks; else packed [.][DP].  W: [.][DP]
+  int64_t ld_rows;
   const float *bias;        // padded to whole tiles with minus infinity
-  const int32_t *label;     // packed
-  const int32_t *list;      // packed row -> row
+  const int32_t *label;     // of the labelled rows, side by side
+  const int32_t *list;      // labelled row -> row
   int32_t C, d;
   float inv_n;
   float *row_loss;          // by row
   bf16_t *dh;               // by row, or NULL
   int64_t ld_dh;
-  float *max, *log, *t;     // packed: the row's maximum, -log2 of its sum, o / l
+  float *max, *log, *t;     // of the labelled rows: the row's maximum, -log2 of its sum, o / l
   float *part;              // [item][wave][DP][32]: sum p W
   float *part_stat;         // [item][3][kOwned]: maximum, others, the label's logit
+  // workgroups from items on write the zeros of the other rows' dh: memory's work, next to the matrix cores'
+  int32_t items, fills;
+  const int32_t *labels;    // by row
+  const uint8_t *mask;
+  int64_t all_rows;
 };
+
+template <int DP>
+__device__ void fill_rows(const RowsArgs &a) {
+  constexpr int per_row = DP / 8;
+  const bool wide = (a.ld_dh & 7) == 0 && (reinterpret_cast<uintptr_t>(a.dh) & 15u) == 0;
+  for (int64_t i = ((int64_t)blockIdx.x - a.items) * 256 + threadIdx.x; i < a.all_rows * per_row; i += (int64_t)a.fills * 256) {
+    const int64_t row = i / per_row;
+    const int k = (int)(i % per_row) * 8;
+    if (k >= a.d || is_labelled(a.labels, a.mask, row, a.C)) continue;
+    bf16_t *dst = a.dh + (size_t)(row * a.ld_dh) + k;
+    if (wide && k + 8 <= a.d) {
+      *reinterpret_cast<bf16x8 *>(dst) = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    } else {
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+        if (k + t < a.d) dst[t] = (bf16_t)0.f;
+    }
+  }
+}
 
 // The end of a row, from its maximum, the others' sum and the label's logit.
 struct RowEnd {
@@ -473,8 +502,8 @@ __device__ inline RowEnd end_row(float m, float others, float zl) {
   return e;
 }
 
-template <int DP, bool GRAD, int IN_REGS>
-__global__ __launch_bounds__(256, 2) void head_rows_kernel(const RowsArgs a) {
+template <int DP, bool GRAD, bool DIRECT, int IN_REGS>
+__global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const RowsArgs a) {
   typedef Geometry<DP> G;
   typedef Owned<DP, IN_REGS> Own;
   __shared__ __attribute__((aligned(1024))) char tile0[G::tile_bytes];
@@ -483,11 +512,17 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(const RowsArgs a) {
   __shared__ __attribute__((aligned(16))) float bias1[kTile];
   __shared__ __attribute__((aligned(16))) char shared[Own::in_lds > 0 ? 4 * Own::in_lds * 1024 : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+  if (GRAD && (int)blockIdx.x >= a.items) {
+    fill_rows<DP>(a);
+    return;
+  }
   const Meta &meta = *a.meta;
   const int splits = meta.splits, item = blockIdx.x, row_tile = item / splits, split = item - row_tile * splits;
   if (row_tile >= meta.row_tiles) return;
   const int first = row_tile * kOwned + wave * 32;
-  const Own own(a.rows, first, wave, lane, shared);
+  // (past the last labelled row: that row once more, whatever it gives is not written)
+  const Own own(DIRECT ? a.rows + (size_t)(a.list[min(first + (lane & 31), meta.n - 1)] * a.ld_rows) : a.rows + (size_t)(first + (lane & 31)) * DP,
+                wave, lane, shared);
   const int label = a.label[first + (lane & 31)];
   f32x16 sum[DP / 32];
   clear<DP>(sum);
@@ -576,36 +611,57 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(const RowsArgs a) {
     }
     return;
   }
-  if (i >= meta.n) return;
+  const bool on = i < meta.n;
   const RowEnd e = end_row(m, others, zl);
-  const int64_t row = a.list[i];
-  if (h == 0) {
+  const int row = on ? a.list[i] : -1;
+  if (on && h == 0) {
     a.row_loss[row] = e.loss;
     a.max[i] = m;
     a.log[i] = e.log;
     a.t[i] = e.t;
   }
   if constexpr (GRAD) {
-    if (a.dh == nullptr) return;
-    const bf16_t *wy = a.W + (size_t)label * DP;
-    bf16_t *dh = a.dh + (size_t)(row * a.ld_dh);
+    // A lane has four columns side by side of its row at a time; through LDS (the tiles are done with) a row's pieces come together: half of
+    // the columns in a pass, 16-byte pieces permuted by the row.
+    const bf16_t *wy = a.W + (size_t)max(label, 0) * DP;
+    const bool wide = (a.ld_dh & 7) == 0 && (reinterpret_cast<uintptr_t>(a.dh) & 15u) == 0;
+    constexpr int half = DP / 2, pieces = half / 8, rows_at_once = 64 / pieces;
+    __syncthreads();
+    lds_char *const room = (wave & 2 ? (lds_char *)tile1 : (lds_char *)tile0) + (wave & 1) * (G::tile_bytes / 2);
 #pragma unroll
-    for (int dt = 0; dt < DP / 32; ++dt)
+    for (int pass = 0; pass < 2; ++pass) {
+      bf16x4 w[DP / 64][4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = 32 * dt + 8 * q + 4 * h;
-        const bf16x4 w = *reinterpret_cast<const bf16x4 *>(wy + c);
-        bf16x4 o;
+      for (int dt = 0; dt < DP / 64; ++dt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[r] = (bf16_t)((sum[dt][4 * q + r] * e.inv - e.t * (float)w[r]) * a.inv_n);
-        if (c + 4 <= a.d && (a.ld_dh & 3) == 0 && (reinterpret_cast<uintptr_t>(a.dh) & 7u) == 0) {
-          *reinterpret_cast<bf16x4 *>(dh + c) = o;
+        for (int q = 0; q < 4; ++q) w[dt][q] = *reinterpret_cast<const bf16x4 *>(wy + pass * half + 32 * dt + 8 * q + 4 * h);
+#pragma unroll
+      for (int dt = 0; dt < DP / 64; ++dt)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          bf16x4 o;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[r] = (bf16_t)((sum[pass * (DP / 64) + dt][4 * q + r] * e.inv - e.t * (float)w[dt][q][r]) * a.inv_n);
+          const int piece = 4 * dt + q, at_row = lane & 31;
+          *reinterpret_cast<LDS_AS bf16x4 *>(room + at_row * DP + ((piece ^ (at_row & (pieces - 1))) << 4) + 8 * h) = o;
+        }
+      // (read by the wave that wrote it)
+#pragma unroll
+      for (int k = 0; k < 32 / rows_at_once; ++k) {
+        const int at_row = k * rows_at_once + lane / pieces, piece = lane % pieces, c = pass * half + piece * 8;
+        const bf16x8 o = *reinterpret_cast<const LDS_AS bf16x8 *>(room + at_row * DP + ((piece ^ (at_row & (pieces - 1))) << 4));
+        const int to = __shfl(row, at_row);
+        if (to < 0) continue;
+        bf16_t *dst = a.dh + (size_t)((int64_t)to * a.ld_dh) + c;
+        if (wide && c + 8 <= a.d) {
+          *reinterpret_cast<bf16x8 *>(dst) = o;
         } else {
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (c + r < a.d) dh[c + r] = o[r];
+          for (int t = 0; t < 8; ++t)
+            if (c + t < a.d) dst[t] = o[t];
         }
       }
+    }
   }
 }
 
@@ -682,21 +738,26 @@ __global__ __launch_bounds__(256) void head_join_kernel(const RowsArgs a) {
 
 struct ClassesArgs {
   const Meta *meta;
-  const bf16_t *rows, *W;
+  const bf16_t *rows, *W;  // as in RowsArgs
+  int64_t ld_rows;
+  const int32_t *list;
   const float *bias;
-  const float *stats;      // packed, of padded_rows each: maximum, -log2 sum, label (int), o / l
+  const float *stats;      // of the labelled rows, padded_rows each: maximum, -log2 sum, label (int), o / l
   int64_t padded_rows;
-  int32_t C, d;
-  int32_t ranges;          // row ranges of the launch
+  int32_t C, d, class_tiles;
   float inv_n;
-  float *dW, *db;          // "+=" (one row range), either may be NULL
-  float *part;             // [range][d][ld_part]
-  float *part_db;          // [range][ld_part]
-  int32_t ld_part;
+  float *dW, *db;          // "+=", either may be NULL
+  float *part;             // [group][2][DP][kOwned]
+  float *part_db;          // [group][2][kOwned]
 };
+// The classes kernel's work, (class tile, row step) pairs in that order, is cut into one run per workgroup (group g: from pair
+// total g / groups on), so that all of them end together: with a workgroup per class tile, 782 class tiles in rounds of 512 took 2.88 ms.  A run's
+// class tiles that are whole are added to dW and db by the kernel; of one that is cut, a group writes its share, in its first slot if
+// its run begins in that tile and in its second if it does not.
+__device__ inline int64_t run_begin(int64_t total, int groups, int g) { return total * g / groups; }
 
-template <int DP, int IN_REGS>
-__global__ __launch_bounds__(256, 2) void head_classes_kernel(const ClassesArgs a) {
+template <int DP, bool DIRECT, int IN_REGS>
+__global__ __launch_bounds__(256, kPerUnit<DP>) void head_classes_kernel(const ClassesArgs a) {
   typedef Geometry<DP> G;
   typedef Owned<DP, IN_REGS> Own;
   struct Stats {
@@ -711,124 +772,189 @@ __global__ __launch_bounds__(256, 2) void head_classes_kernel(const ClassesArgs 
   __shared__ __attribute__((aligned(16))) Stats stats1;
   __shared__ __attribute__((aligned(16))) char shared[Own::in_lds > 0 ? 4 * Own::in_lds * 1024 : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-  const Meta &meta = *a.meta;
-  const int range = blockIdx.x % a.ranges, class_tile = blockIdx.x / a.ranges;
-  if (range >= meta.ranges) return;
-  const int first = class_tile * kOwned + wave * 32, c = first + (lane & 31);
-  const bool idle = first >= a.C;  // this wave has no classes; it still loads
-  const Own own(a.W, first, wave, lane, shared);
-  const float bias = a.bias[c];
-  f32x16 sum[DP / 32];
-  clear<DP>(sum);
-  float g_sum = 0.f, g_low = 0.f;
+  const int row_steps = a.meta->row_steps, groups = a.meta->groups, n = a.meta->n, group = blockIdx.x;
+  if (group >= groups) return;
+  const int64_t total = (int64_t)a.class_tiles * row_steps, run0 = run_begin(total, groups, group), run1 = run_begin(total, groups, group + 1);
   Places<DP> at(wave, lane);
-  const int tiles = (meta.n + kTile - 1) / kTile, per = meta.rows_per / kTile, begin = range * per, end = min(tiles, begin + per);
+  int32_t index[DIRECT ? G::loads : 1];  // of the rows that this lane loads next
+  auto look_up = [&](int tile) {
+    if constexpr (DIRECT) {
+#pragma unroll
+      for (int q = 0; q < G::loads; ++q) index[q] = a.list[min(tile * kTile + q * 4 * G::rows_per_load + wave * G::rows_per_load + lane / G::chunks, n - 1)];
+    }
+  };
   auto load = [&](int tile, lds_char *dst, Stats *st) {
-    load_tile<DP>(a.rows + (size_t)tile * kTile * DP, dst, wave, at.load);
+    if constexpr (DIRECT) {
+      // (rows past the last labelled one: that one again, times g = 0)
+#pragma unroll
+      for (int q = 0; q < G::loads; ++q) {
+        constexpr int step = 4 * G::rows_per_load;
+        const uint32_t turn = (lds_swizzle<DP>(q * step) ^ lds_swizzle<DP>(0)) << 4;
+        load_lds16(reinterpret_cast<const char *>(a.rows + (size_t)(index[q] * a.ld_rows)) + ((at.load ^ turn) & (G::row_bytes - 1)),
+                   dst + q * step * G::row_bytes + wave * 1024);
+      }
+    } else {
+      load_tile<DP>(a.rows + (size_t)tile * kTile * DP, dst, wave, at.load);
+    }
     if (threadIdx.x < kTile)
       load_lds16(a.stats + (size_t)(threadIdx.x >> 3) * a.padded_rows + (size_t)tile * kTile + (threadIdx.x & 7) * 4, (lds_char *)st);
   };
-  auto step = [&](int tile, const lds_char *now, const Stats *st, lds_char *next, Stats *next_st) {
-    wait_tile();
-    if (tile + 1 < end) load(tile + 1, next, next_st);
-    if (idle) return;
-    at.renew();
-    // (the bias first, as in the rows kernel: the same logits to the last bit, so that large ones meet their own maximum)
-    f32x16 z;
+  for (int64_t pair = run0; pair < run1;) {
+    const int class_tile = (int)(pair / row_steps), begin = (int)(pair - (int64_t)class_tile * row_steps);
+    const int end = (int)min((int64_t)row_steps, begin + (run1 - pair));
+    const int first = class_tile * kOwned + wave * 32, c = first + (lane & 31);
+    const bool idle = first >= a.C;  // this wave has no classes; it still loads
+    __syncthreads();  // the last class tile's streamed rows are done with
+    look_up(begin);
+    const Own own(a.W + (size_t)c * DP, wave, lane, shared);
+    const float bias = a.bias[c];
+    f32x16 sum[DP / 32];
+    clear<DP>(sum);
+    float g_sum = 0.f, g_low = 0.f;
+    load(begin, (lds_char *)tile0, &stats0);
+    look_up(begin + 1);
+    auto step = [&](int tile, const lds_char *now, const Stats *st, lds_char *next, Stats *next_st) {
+      wait_tile();
+      if (tile + 1 < end) {
+        load(tile + 1, next, next_st);
+        look_up(tile + 2);
+      }
+      if (idle) return;
+      at.renew();
+      // (the bias first, as in the rows kernel: the same logits to the last bit, so that large ones meet their own maximum)
+      f32x16 z;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = bias;
+      for (int i = 0; i < 16; ++i) z[i] = bias;
 #pragma unroll
-    for (int ks = 0; ks < DP / 16; ++ks) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(first_operand<DP>(now, at.first, ks), own(ks), z, 0, 0, 0);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x4 m = *reinterpret_cast<const f32x4 *>(st->max + 8 * q + 4 * h), l = *reinterpret_cast<const f32x4 *>(st->log + 8 * q + 4 * h);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) z[4 * q + r] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + r] - m[r], kLog2e, l[r]));
-    }
-    if (__any((uint32_t)(st->label[lane & 31] - first) < 32u)) {
+      for (int ks = 0; ks < DP / 16; ++ks) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(first_operand<DP>(now, at.first, ks), own(ks), z, 0, 0, 0);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const i32x4 y = *reinterpret_cast<const i32x4 *>(st->label + 8 * q + 4 * h);
-        const f32x4 t = *reinterpret_cast<const f32x4 *>(st->t + 8 * q + 4 * h);
+        const f32x4 m = *reinterpret_cast<const f32x4 *>(st->max + 8 * q + 4 * h), l = *reinterpret_cast<const f32x4 *>(st->log + 8 * q + 4 * h);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) z[4 * q + r] = y[r] == c ? -t[r] : z[4 * q + r];
+        for (int r = 0; r < 4; ++r) z[4 * q + r] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + r] - m[r], kLog2e, l[r]));
       }
-    }
-    // db takes g as it is; its long sum is compensated
-    float part = 0.f;
+      if (__any((uint32_t)(st->label[lane & 31] - first) < 32u)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) part += z[i];
-    const float y = part - g_low, s = g_sum + y;
-    g_low = (s - g_sum) - y;
-    g_sum = s;
-    bf16x8 high[2], low[2];  // g = high + low to 16 bits
+        for (int q = 0; q < 4; ++q) {
+          const i32x4 y = *reinterpret_cast<const i32x4 *>(st->label + 8 * q + 4 * h);
+          const f32x4 t = *reinterpret_cast<const f32x4 *>(st->t + 8 * q + 4 * h);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      high[i >> 3][i & 7] = (bf16_t)z[i];
-      low[i >> 3][i & 7] = (bf16_t)(z[i] - (float)high[i >> 3][i & 7]);
+          for (int r = 0; r < 4; ++r) z[4 * q + r] = y[r] == c ? -t[r] : z[4 * q + r];
+        }
+      }
+      // db takes g as it is; its long sum is compensated
+      float part = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) part += z[i];
+      const float y = part - g_low, s = g_sum + y;
+      g_low = (s - g_sum) - y;
+      g_sum = s;
+      bf16x8 high[2], low[2];  // g = high + low to 16 bits
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        high[i >> 3][i & 7] = (bf16_t)z[i];
+        low[i >> 3][i & 7] = (bf16_t)(z[i] - (float)high[i >> 3][i & 7]);
+      }
+#pragma unroll
+      for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const bf16x8 x = lds_turned<DP>(now, at.second, dt, t);
+          sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, high[t], sum[dt], 0, 0, 0);
+          sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, low[t], sum[dt], 0, 0, 0);
+        }
+    };
+    for (int tile = begin; tile < end; tile += 2) {
+      step(tile, (const lds_char *)tile0, &stats0, (lds_char *)tile1, &stats1);
+      if (tile + 1 < end) step(tile + 1, (const lds_char *)tile1, &stats1, (lds_char *)tile0, &stats0);
     }
+    const bool whole = begin == 0 && end == row_steps;
+    const int64_t slot = 2 * (int64_t)group + (pair == run0 ? 0 : 1);
+    pair += end - begin;
+    if (c >= a.C) continue;
+    g_sum += __shfl_xor(g_sum, 32);
+    if (a.db != nullptr && h == 0) {
+      if (whole)
+        a.db[c] += g_sum * a.inv_n;
+      else
+        a.part_db[slot * kOwned + wave * 32 + (lane & 31)] = g_sum;
+    }
+    if (a.dW == nullptr) continue;
+    float *to = whole ? a.dW + c : a.part + slot * DP * kOwned + wave * 32 + (lane & 31);
+    int64_t stride = whole ? a.C : kOwned;
+    int d = a.d;
+    asm volatile("" : "+s"(stride), "+s"(d));  // (or the compiler makes all addresses ahead of the loop, and spills)
+    to += 4 * h * stride;
 #pragma unroll
     for (int dt = 0; dt < DP / 32; ++dt)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const bf16x8 x = lds_turned<DP>(now, at.second, dt, t);
-        sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, high[t], sum[dt], 0, 0, 0);
-        sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, low[t], sum[dt], 0, 0, 0);
+      for (int t = 0; t < 16; ++t) {
+        const int k = 32 * dt + 8 * (t >> 2) + (t & 3);
+        if (k + 4 * h >= d) continue;
+        if (whole)
+          to[k * stride] += sum[dt][t] * a.inv_n;
+        else
+          to[k * stride] = sum[dt][t];
       }
-  };
-  if (begin < end) load(begin, (lds_char *)tile0, &stats0);
-  for (int tile = begin; tile < end; tile += 2) {
-    step(tile, (const lds_char *)tile0, &stats0, (lds_char *)tile1, &stats1);
-    if (tile + 1 < end) step(tile + 1, (const lds_char *)tile1, &stats1, (lds_char *)tile0, &stats0);
   }
-  if (c >= a.C) return;
-  g_sum += __shfl_xor(g_sum, 32);
-  const bool whole = a.ranges == 1;
-  if (a.db != nullptr && h == 0) {
-    if (whole)
-      a.db[c] += g_sum * a.inv_n;
-    else
-      a.part_db[(size_t)range * a.ld_part + c] = g_sum;
-  }
-  if (a.dW == nullptr) return;
-#pragma unroll
-  for (int dt = 0; dt < DP / 32; ++dt)
-#pragma unroll
-    for (int t = 0; t < 16; ++t) {
-      const int k = 32 * dt + 8 * (t >> 2) + 4 * h + (t & 3);
-      if (k >= a.d) continue;
-      if (whole)
-        a.dW[(size_t)k * a.C + c] += sum[dt][t] * a.inv_n;
-      else
-        a.part[((size_t)range * a.d + k) * a.ld_part + c] = sum[dt][t];
-    }
 }
 
-// dW[k][c] += inv_n * sum over the row ranges, in their order; row d is db.  64 outputs per workgroup, four runs of ranges side by side.
+// The shares of the class tiles that were cut, in the order of their rows.  A workgroup: 64 classes, four rows k of dW (row d is db) side
+// by side, or one row whose shares are added up in four runs where there are many.
+template <int DP>
 __global__ __launch_bounds__(256) void head_reduce_kernel(const ClassesArgs a) {
   __shared__ float red[4][64];
-  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6, ranges = a.meta->ranges, k = blockIdx.y;
-  const int c = blockIdx.x * 64 + tx;
-  const bool bias = k == a.d;
-  float *dst = bias ? a.db : a.dW == nullptr ? nullptr : a.dW + (size_t)k * a.C;
-  if (dst == nullptr) return;  // whole workgroup
-  const float *src = bias ? a.part_db : a.part + (size_t)k * a.ld_part;
-  const size_t stride = bias ? (size_t)a.ld_part : (size_t)a.d * a.ld_part;
-  const int per = (ranges + 3) / 4, r0 = ty * per, r1 = min(ranges, r0 + per);
-  float s = 0.f;
-  if (c < a.C) {
-    int r = r0;
-    for (; r + 8 <= r1; r += 8) {
-      float v[8];
-#pragma unroll
-      for (int t = 0; t < 8; ++t) v[t] = src[(size_t)(r + t) * stride + c];
-      s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-    }
-    for (; r < r1; ++r) s += src[(size_t)r * stride + c];
+  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6, row_steps = a.meta->row_steps, groups = a.meta->groups;
+  const int class_tile = blockIdx.x >> 1, in_tile = (blockIdx.x & 1) * 64 + tx, c = class_tile * kOwned + in_tile;
+  if (groups == 0) return;
+  const int64_t total = (int64_t)a.class_tiles * row_steps, from = (int64_t)class_tile * row_steps, to = from + row_steps;
+  // the groups that have the tile's first and last pair
+  auto owner = [&](int64_t pair) {
+    int g = (int)min((int64_t)groups - 1, (pair * groups + groups - 1) / total);
+    while (run_begin(total, groups, g) > pair) --g;
+    while (g + 1 < groups && run_begin(total, groups, g + 1) <= pair) ++g;
+    return g;
+  };
+  const int g0 = owner(from), g1 = owner(to - 1);
+  if (g0 == g1) return;  // whole workgroup: nothing was cut
+  auto share = [&](int k, int g) {
+    const int64_t slot = 2 * (int64_t)g + (run_begin(total, groups, g) >= from ? 0 : 1);
+    return k == a.d ? a.part_db[slot * kOwned + in_tile] : a.part[(slot * DP + k) * kOwned + in_tile];
+  };
+  auto wanted = [&](int k) { return k < a.d ? a.dW != nullptr : k == a.d && a.db != nullptr; };
+  auto add = [&](int k, float x) {
+    float *dst = k == a.d ? a.db + c : a.dW + (size_t)k * a.C + c;
+    *dst += a.inv_n * x;
+  };
+  const int shares = g1 - g0 + 1;
+  if (shares <= 8) {
+    for (int k = blockIdx.y * 4 + ty; k <= a.d; k += gridDim.y * 4)
+      if (wanted(k) && c < a.C) {
+        float x = 0.f;
+        for (int g = g0; g <= g1; ++g) x += share(k, g);
+        add(k, x);
+      }
+    return;
   }
-  red[ty][tx] = s;
-  __syncthreads();
-  if (ty == 0 && c < a.C) dst[c] += a.inv_n * ((red[0][tx] + red[1][tx]) + (red[2][tx] + red[3][tx]));
+  for (int k = blockIdx.y; k <= a.d; k += gridDim.y) {
+    if (!wanted(k)) continue;  // whole workgroup
+    const int per = (shares + 3) / 4, r0 = g0 + ty * per, r1 = min(g1 + 1, r0 + per);
+    float x = 0.f;
+    if (c < a.C) {
+      int g = r0;
+      for (; g + 8 <= r1; g += 8) {
+        float v[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = share(k, g + t);
+        x += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+      }
+      for (; g < r1; ++g) x += share(k, g);
+    }
+    red[ty][tx] = x;
+    __syncthreads();
+    if (ty == 0 && c < a.C) add(k, (red[0][tx] + red[1][tx]) + (red[2][tx] + red[3][tx]));
+    __syncthreads();
+  }
 }
 
 struct PrepareArgs {
@@ -848,9 +974,7 @@ struct PrepareArgs {
   float *bias;
   float *stats;           // maximum, -log2 sum, label, t
   float *row_loss;
-  bf16_t *dh;
-  int64_t ld_dh;
-  int32_t max_splits, ranges;
+  int32_t max_splits, round;
 };
 
 // Workgroups [0, n_counts) count labelled rows; the others turn the weights, 64 x 64 at a time, and pad the biases.
@@ -933,67 +1057,47 @@ __global__ __launch_bounds__(256) void head_list_kernel(const PrepareArgs a) {
     const int real = (tiles + per - 1) / per;
     const int64_t items = (int64_t)m.row_tiles * real;
     const bool may = tried <= a.max_splits && (real == 1 || items <= kRowItems);
-    uint64_t cost = may ? (uint64_t)(((items + kRound - 1) / kRound * (per + (real > 1 ? 8 : 4))) << 6 | lane) : ~0ull;  // the fewest of equals
+    uint64_t cost = may ? (uint64_t)(((items + a.round - 1) / a.round * (per + (real > 1 ? 8 : 4))) << 6 | lane) : ~0ull;  // the fewest of equals
     uint64_t least = cost;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) least = min(least, (uint64_t)__shfl_xor((unsigned long long)least, o));
     m.splits = __shfl(real, (int)(least & 63));
     m.tiles_per = __shfl(per, (int)(least & 63));
-    const int row_steps = (at + kTile - 1) / kTile;
-    per = max((row_steps + a.ranges - 1) / a.ranges, 1);
-    m.rows_per = per * kTile;
-    m.ranges = (row_steps + per - 1) / per;
+    m.row_steps = (at + kTile - 1) / kTile;
+    // runs of four steps at least
+    m.groups = (int32_t)min((int64_t)a.round, ((int64_t)(a.padded_classes / kOwned) * m.row_steps + 3) / 4);
     if (lane == 0) *a.meta = m;
+    // what stands behind the last labelled row, up to a whole workgroup's
+    for (int i = at + lane; i < m.row_tiles * kOwned; i += 64) {
+      a.stats[i] = INFINITY;
+      a.stats[a.padded_rows + i] = a.stats[3 * a.padded_rows + i] = 0.f;
+      label[i] = -1;
+    }
   }
 }
 
-// The labelled rows side by side, zeros from d to DP and behind the last of them up to whole workgroups; zero rows of dh for the others.
-// A thread per eight columns.
-__global__ __launch_bounds__(256) void head_pack_kernel(const PrepareArgs a, int64_t pack_blocks) {
+// The labelled rows side by side, zeros from d to DP and behind the last of them up to whole workgroups.  A thread per eight columns.
+__global__ __launch_bounds__(256) void head_pack_kernel(const PrepareArgs a) {
   const int per_row = a.DP / 8;
-  if ((int64_t)blockIdx.x < pack_blocks) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / per_row;
-    const int k = (threadIdx.x % per_row) * 8, n = a.meta->n;
-    if (i >= (int64_t)(n + kOwned - 1) / kOwned * kOwned) return;
-    bf16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (i < n) {
-      const bf16_t *src = a.h + (size_t)(a.list[i] * a.ld_h) + k;
-      if (k + 8 <= a.d && (a.ld_h & 7) == 0 && (reinterpret_cast<uintptr_t>(a.h) & 15u) == 0) {
-        v = *reinterpret_cast<const bf16x8 *>(src);
-      } else {
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-          if (k + t < a.d) v[t] = src[t];
-      }
-    } else if (k == 0) {
-      a.stats[i] = INFINITY;
-      reinterpret_cast<int32_t *>(a.stats + 2 * a.padded_rows)[i] = -1;
-      a.stats[a.padded_rows + i] = a.stats[3 * a.padded_rows + i] = 0.f;
-    }
-    *reinterpret_cast<bf16x8 *>(a.packed + (size_t)i * a.DP + k) = v;
-    return;
-  }
-  const int64_t i = (((int64_t)blockIdx.x - pack_blocks) * 256 + threadIdx.x) / per_row;
-  const int k = (threadIdx.x % per_row) * 8;
-  if (i >= a.rows || k >= a.d || is_labelled(a.labels, a.mask, i, a.C)) return;
-  bf16_t *dst = a.dh + (size_t)(i * a.ld_dh) + k;
-  if (k + 8 <= a.d && (a.ld_dh & 7) == 0 && (reinterpret_cast<uintptr_t>(a.dh) & 15u) == 0) {
-    *reinterpret_cast<bf16x8 *>(dst) = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
-  } else {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / per_row;
+  const int k = (threadIdx.x % per_row) * 8, n = a.meta->n;
+  if (i >= (int64_t)(n + kOwned - 1) / kOwned * kOwned) return;
+  bf16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (i < n) {
+    const bf16_t *src = a.h + (size_t)(a.list[i] * a.ld_h) + k;
 #pragma unroll
     for (int t = 0; t < 8; ++t)
-      if (k + t < a.d) dst[t] = (bf16_t)0.f;
+      if (k + t < a.d) v[t] = src[t];
   }
+  *reinterpret_cast<bf16x8 *>(a.packed + (size_t)i * a.DP + k) = v;
 }
 
 struct FusedPlan {
-  int64_t rows = 0, padded_rows = 0, max_items = 0, pack_blocks = 0;
-  int d = 0, C = 0, DP = 0, padded_classes = 0, n_counts = 0, max_splits = 1, ranges = 1, class_tiles = 0, ld_part = 0;
-  bool grads = false;
+  int64_t rows = 0, padded_rows = 0, max_items = 0;
+  int d = 0, C = 0, DP = 0, padded_classes = 0, n_counts = 0, max_splits = 1, class_tiles = 0;
   size_t counts = 0, meta = 0, list = 0, stats = 0, packed = 0, Wt = 0, bias = 0, part = 0, part_stat = 0, part_dW = 0, part_db = 0, total = 0;
 };
 constexpr int64_t kFusedRows = (int64_t)1 << 20;  // of a slab: their packed copy is half a gigabyte at most
-constexpr size_t kRangeBytes = (size_t)256 << 20;  // partial sums of the classes kernel
 
 bool fused_takes(int d, int dtype) { return dtype == GNNSTAGE_BF16 && d <= 256; }
 
@@ -1003,31 +1107,15 @@ FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads) {
   p.rows = rows;
   p.d = d;
   p.C = C;
-  p.grads = grads;
   p.DP = d <= 64 ? 64 : d <= 128 ? 128 : 256;
   const int64_t row_tiles = std::max<int64_t>(1, (rows + kOwned - 1) / kOwned);
   p.padded_rows = row_tiles * kOwned;
   p.class_tiles = (C + kOwned - 1) / kOwned;
   p.padded_classes = p.class_tiles * kOwned;
   p.n_counts = (int)std::max<int64_t>(1, (rows + kMetaBlock - 1) / kMetaBlock);
-  p.pack_blocks = p.padded_rows * (p.DP / 8) / 256;
   // class ranges of eight tiles at least
   p.max_splits = std::max(1, std::min(kMaxSplits, (C + 8 * kTile - 1) / (8 * kTile)));
   p.max_items = std::min(row_tiles * p.max_splits, std::max<int64_t>(row_tiles, kRowItems));
-  // row ranges of the classes kernel: rounds of workgroups filled as far as the partial sums' room allows
-  const int64_t steps = std::max<int64_t>(1, (rows + kTile - 1) / kTile);
-  p.ld_part = round_up(C, 32);
-  const size_t bytes = sizeof(float) * (size_t)d * p.ld_part;
-  double best = -1;
-  for (int r = 1; r <= 512 && r <= steps && (r == 1 || (size_t)r * bytes <= kRangeBytes); ++r) {
-    const int64_t items = (int64_t)p.class_tiles * r;
-    const int64_t per = (steps + r - 1) / r;
-    const double cost = (double)((items + kRound - 1) / kRound) * (double)(per + (r > 1 ? 8 : 4));
-    if (best < 0 || cost < best) {
-      best = cost;
-      p.ranges = r;
-    }
-  }
   size_t off = 0;
   auto take = [&](size_t b) {
     const size_t at = off;
@@ -1038,14 +1126,16 @@ FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads) {
   p.meta = take(sizeof(Meta));
   p.list = take(sizeof(int32_t) * (size_t)p.padded_rows);
   p.stats = take(4 * sizeof(float) * (size_t)p.padded_rows);
+  // (also where the rows can be read as they are: whether they can is not known from their sizes)
   p.packed = take(2 * (size_t)p.padded_rows * p.DP);
   p.Wt = take(2 * (size_t)p.padded_classes * p.DP);
   p.bias = take(sizeof(float) * (size_t)p.padded_classes);
   const int64_t part_items = p.max_splits > 1 ? std::min<int64_t>(p.max_items, kRowItems) : 0;
   p.part_stat = take(sizeof(float) * 3 * kOwned * (size_t)part_items);
   p.part = take(grads ? sizeof(float) * (size_t)kOwned * p.DP * (size_t)part_items : 0);
-  p.part_dW = take(grads && p.ranges > 1 ? bytes * (size_t)p.ranges : 0);
-  p.part_db = take(grads && p.ranges > 1 ? sizeof(float) * (size_t)p.ld_part * p.ranges : 0);
+  const int64_t groups = grads ? std::min<int64_t>(round_of(p.DP), ((int64_t)p.class_tiles * ((rows + kTile - 1) / kTile) + 3) / 4) : 0;
+  p.part_dW = take(sizeof(float) * 2 * (size_t)groups * p.DP * kOwned);
+  p.part_db = take(sizeof(float) * 2 * (size_t)groups * kOwned);
   p.total = off;
   return p;
 }
@@ -1054,7 +1144,7 @@ FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads) {
 constexpr int kRowsInRegs = 12, kClassesInRegs = 8;  // width 256
 
 // a slab of at most p.rows rows; first: the weights are not there yet
-template <int DP>
+template <int DP, bool DIRECT>
 int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipStream_t s) {
   auto at = [&](size_t off) { return c.ws + off; };
   PrepareArgs a{};
@@ -1079,22 +1169,23 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   a.bias = reinterpret_cast<float *>(at(p.bias));
   a.stats = reinterpret_cast<float *>(at(p.stats));
   a.row_loss = c.row_loss;
-  a.dh = static_cast<bf16_t *>(c.dh);
-  a.ld_dh = c.ld_dh;
   a.max_splits = p.max_splits;
-  a.ranges = p.ranges;
+  a.round = round_of(DP);
   const unsigned turn_blocks = first ? (unsigned)(p.padded_classes / 64 * (DP / 64)) : 0;
   hipLaunchKernelGGL(head_count_kernel, dim3((unsigned)a.n_counts + turn_blocks), dim3(256), 0, s, a);
   HEAD_TRY(hipGetLastError());
   hipLaunchKernelGGL(head_list_kernel, dim3((unsigned)a.n_counts), dim3(256), 0, s, a);
   HEAD_TRY(hipGetLastError());
-  const int64_t zero_blocks = c.dh ? (rows * (DP / 8) + 255) / 256 : 0;
-  hipLaunchKernelGGL(head_pack_kernel, dim3((unsigned)(p.pack_blocks + zero_blocks)), dim3(256), 0, s, a, p.pack_blocks);
-  HEAD_TRY(hipGetLastError());
+  const int64_t row_tiles = (rows + kOwned - 1) / kOwned;
+  if (!DIRECT) {
+    hipLaunchKernelGGL(head_pack_kernel, dim3((unsigned)(row_tiles * kOwned * (DP / 8) / 256)), dim3(256), 0, s, a);
+    HEAD_TRY(hipGetLastError());
+  }
 
   RowsArgs r{};
   r.meta = a.meta;
-  r.rows = a.packed;
+  r.rows = DIRECT ? a.h : a.packed;
+  r.ld_rows = c.ld_h;
   r.W = a.Wt;
   r.bias = a.bias;
   r.label = reinterpret_cast<const int32_t *>(a.stats + 2 * p.padded_rows);
@@ -1103,7 +1194,7 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   r.d = p.d;
   r.inv_n = c.inv_n;
   r.row_loss = c.row_loss;
-  r.dh = a.dh;
+  r.dh = static_cast<bf16_t *>(c.dh);
   r.ld_dh = c.ld_dh;
   r.max = a.stats;
   r.log = a.stats + p.padded_rows;
@@ -1112,11 +1203,16 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   r.part_stat = reinterpret_cast<float *>(at(p.part_stat));
   constexpr int kAll = DP / 16;
   const bool sums = c.dh != nullptr;
-  hipLaunchKernelGGL((sums ? head_rows_kernel<DP, true, (kAll < kRowsInRegs ? kAll : kRowsInRegs)> : head_rows_kernel<DP, false, kAll>),
-                     dim3((unsigned)p.max_items), dim3(256), 0, s, r);
+  r.items = (int32_t)std::min(row_tiles * p.max_splits, std::max<int64_t>(row_tiles, kRowItems));
+  r.fills = sums ? (int32_t)std::min<int64_t>(1024, (rows * (DP / 8) + 1023) / 1024) : 0;
+  r.labels = c.labels;
+  r.mask = c.mask;
+  r.all_rows = rows;
+  hipLaunchKernelGGL((sums ? head_rows_kernel<DP, true, DIRECT, (kAll < kRowsInRegs ? kAll : kRowsInRegs)> : head_rows_kernel<DP, false, DIRECT, kAll>),
+                     dim3((unsigned)(r.items + r.fills)), dim3(256), 0, s, r);
   HEAD_TRY(hipGetLastError());
   if (p.max_splits > 1) {
-    const unsigned blocks = 4u * (unsigned)std::min<int64_t>(p.padded_rows / kOwned, kRowItems);
+    const unsigned blocks = 4u * (unsigned)std::min<int64_t>(row_tiles, kRowItems);
     hipLaunchKernelGGL((sums ? head_join_kernel<DP, true> : head_join_kernel<DP, false>), dim3(blocks, sums ? (unsigned)((p.d + kJoinColumns - 1) / kJoinColumns) : 1u),
                        dim3(256), 0, s, r);
     HEAD_TRY(hipGetLastError());
@@ -1124,28 +1220,34 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   if (!c.dW && !c.db) return hipSuccess;
   ClassesArgs k{};
   k.meta = a.meta;
-  k.rows = a.packed;
+  k.rows = r.rows;
+  k.ld_rows = c.ld_h;
+  k.list = a.list;
   k.W = a.Wt;
   k.bias = a.bias;
   k.stats = a.stats;
   k.padded_rows = p.padded_rows;
   k.C = p.C;
   k.d = p.d;
-  k.ranges = p.ranges;
+  k.class_tiles = p.class_tiles;
   k.inv_n = c.inv_n;
   k.dW = c.dW;
   k.db = c.db;
   k.part = reinterpret_cast<float *>(at(p.part_dW));
   k.part_db = reinterpret_cast<float *>(at(p.part_db));
-  k.ld_part = p.ld_part;
-  hipLaunchKernelGGL((head_classes_kernel<DP, (kAll < kClassesInRegs ? kAll : kClassesInRegs)>), dim3((unsigned)(p.class_tiles * p.ranges)),
-                     dim3(256), 0, s, k);
+  const int64_t groups = std::min<int64_t>(round_of(p.DP), ((int64_t)p.class_tiles * ((rows + kTile - 1) / kTile) + 3) / 4);  // at most
+  hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, (kAll < kClassesInRegs ? kAll : kClassesInRegs)>), dim3((unsigned)groups), dim3(256), 0, s, k);
   HEAD_TRY(hipGetLastError());
-  if (p.ranges > 1) {
-    hipLaunchKernelGGL(head_reduce_kernel, dim3((unsigned)((p.C + 63) / 64), (unsigned)p.d + 1), dim3(256), 0, s, k);
-    HEAD_TRY(hipGetLastError());
-  }
-  return hipSuccess;
+  // many shares of few class tiles: a workgroup per row of dW; few shares of many: some rows each
+  const unsigned gy = p.class_tiles < 64 ? (unsigned)p.d + 1 : 8u;
+  hipLaunchKernelGGL(head_reduce_kernel<DP>, dim3(2u * (unsigned)p.class_tiles, gy), dim3(256), 0, s, k);
+  return (int)hipGetLastError();
+}
+template <int DP>
+int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipStream_t s) {
+  // rows of the very width in whole 16-byte pieces are read where they are, others from a packed copy
+  const bool direct = p.d == DP && c.ld_h % 8 == 0 && (reinterpret_cast<uintptr_t>(c.h) & 15u) == 0;
+  return direct ? run_fused<DP, true>(p, c, rows, first, s) : run_fused<DP, false>(p, c, rows, first, s);
 }
 
 size_t workspace_bytes_of(const Plan &p) {
