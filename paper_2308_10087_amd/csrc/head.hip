@@ -473,17 +473,28 @@ template <int DP>
 __device__ void fill_rows(const RowsArgs &a) {
   constexpr int per_row = DP / 8;
   const bool wide = (a.ld_dh & 7) == 0 && (reinterpret_cast<uintptr_t>(a.dh) & 15u) == 0;
-  for (int64_t i = ((int64_t)blockIdx.x - a.items) * 256 + threadIdx.x; i < a.all_rows * per_row; i += (int64_t)a.fills * 256) {
-    const int64_t row = i / per_row;
-    const int k = (int)(i % per_row) * 8;
-    if (k >= a.d || is_labelled(a.labels, a.mask, row, a.C)) continue;
-    bf16_t *dst = a.dh + (size_t)(row * a.ld_dh) + k;
-    if (wide && k + 8 <= a.d) {
-      *reinterpret_cast<bf16x8 *>(dst) = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
-    } else {
+  const int64_t step = (int64_t)a.fills * 256, all = a.all_rows * per_row;
+  // (eight pieces' labels are asked for at a time: no read passes the writes in front of it)
+  for (int64_t i0 = ((int64_t)blockIdx.x - a.items) * 256 + threadIdx.x; i0 < all; i0 += 8 * step) {
+    bool zero[8];
 #pragma unroll
-      for (int t = 0; t < 8; ++t)
-        if (k + t < a.d) dst[t] = (bf16_t)0.f;
+    for (int u = 0; u < 8; ++u) {
+      const int64_t row = min(i0 + u * step, all - 1) / per_row;
+      zero[u] = (a.mask != nullptr && a.mask[row] == 0) | ((uint32_t)a.labels[row] >= (uint32_t)a.C);
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t i = i0 + u * step;
+      const int k = (int)(i % per_row) * 8;
+      if (i >= all || k >= a.d || !zero[u]) continue;
+      bf16_t *dst = a.dh + (size_t)(i / per_row * a.ld_dh) + k;
+      if (wide && k + 8 <= a.d) {
+        *reinterpret_cast<bf16x8 *>(dst) = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+      } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if (k + t < a.d) dst[t] = (bf16_t)0.f;
+      }
     }
   }
 }
@@ -521,9 +532,6 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
   if (row_tile >= meta.row_tiles) return;
   const int first = row_tile * kOwned + wave * 32;
   // (past the last labelled row: that row once more, whatever it gives is not written)
-  const Own own(DIRECT ? a.rows + (size_t)(a.list[min(first + (lane & 31), meta.n - 1)] * a.ld_rows) : a.rows + (size_t)(first + (lane & 31)) * DP,
-                wave, lane, shared);
-  const int label = a.label[first + (lane & 31)];
   f32x16 sum[DP / 32];
   clear<DP>(sum);
   float m = kNoMax, others = 0.f, zl = -INFINITY;
@@ -533,6 +541,11 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
     load_tile<DP>(a.W + (size_t)tile * kTile * DP, dst, wave, at.load);
     if (threadIdx.x < kTile / 4) load_lds16(a.bias + (size_t)tile * kTile + threadIdx.x * 4, (lds_char *)bias);
   };
+  if (begin < end) load(begin, (lds_char *)tile0, bias0);
+  // (past the last labelled row: that row once more, whatever it gives is not written)
+  const Own own(DIRECT ? a.rows + (size_t)(a.list[min(first + (lane & 31), meta.n - 1)] * a.ld_rows) : a.rows + (size_t)(first + (lane & 31)) * DP,
+                wave, lane, shared);
+  const int label = a.label[first + (lane & 31)];
   auto step = [&](int tile, const lds_char *now, const float *bias, lds_char *next, float *next_bias) {
     wait_tile();
     if (tile + 1 < end) load(tile + 1, next, next_bias);
@@ -587,7 +600,6 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
           sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_turned<DP>(now, at.second, dt, t), p[t], sum[dt], 0, 0, 0);
     }
   };
-  if (begin < end) load(begin, (lds_char *)tile0, bias0);
   for (int tile = begin; tile < end; tile += 2) {
     step(tile, (const lds_char *)tile0, bias0, (lds_char *)tile1, bias1);
     if (tile + 1 < end) step(tile + 1, (const lds_char *)tile1, bias1, (lds_char *)tile0, bias0);
@@ -882,20 +894,34 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_classes_kernel(const C
     if (a.dW == nullptr) continue;
     float *to = whole ? a.dW + c : a.part + slot * DP * kOwned + wave * 32 + (lane & 31);
     int64_t stride = whole ? a.C : kOwned;
-    int d = a.d;
-    asm volatile("" : "+s"(stride), "+s"(d));  // (or the compiler makes all addresses ahead of the loop, and spills)
+    const int d = DIRECT ? DP : a.d;
+    asm volatile("" : "+s"(stride));  // (or the compiler makes all addresses ahead of the loop, and spills)
     to += 4 * h * stride;
+    if (whole) {
+      // (16 at a time: what is added to has to be read, and no read passes the writes in front of it)
 #pragma unroll
-    for (int dt = 0; dt < DP / 32; ++dt)
+      for (int dt = 0; dt < DP / 32; ++dt) {
+        float old[16];
 #pragma unroll
-      for (int t = 0; t < 16; ++t) {
-        const int k = 32 * dt + 8 * (t >> 2) + (t & 3);
-        if (k + 4 * h >= d) continue;
-        if (whole)
-          to[k * stride] += sum[dt][t] * a.inv_n;
-        else
-          to[k * stride] = sum[dt][t];
+        for (int t = 0; t < 16; ++t) {
+          const int k = 32 * dt + 8 * (t >> 2) + (t & 3);
+          old[t] = k + 4 * h < d ? to[k * stride] : 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+          const int k = 32 * dt + 8 * (t >> 2) + (t & 3);
+          if (k + 4 * h < d) to[k * stride] = old[t] + sum[dt][t] * a.inv_n;
+        }
       }
+    } else {
+#pragma unroll
+      for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+          const int k = 32 * dt + 8 * (t >> 2) + (t & 3);
+          if (k + 4 * h < d) to[k * stride] = sum[dt][t];
+        }
+    }
   }
 }
 
@@ -917,8 +943,9 @@ __global__ __launch_bounds__(256) void head_reduce_kernel(const ClassesArgs a) {
   };
   const int g0 = owner(from), g1 = owner(to - 1);
   if (g0 == g1) return;  // whole workgroup: nothing was cut
+  const int first_slot = run_begin(total, groups, g0) >= from ? 0 : 1;
   auto share = [&](int k, int g) {
-    const int64_t slot = 2 * (int64_t)g + (run_begin(total, groups, g) >= from ? 0 : 1);
+    const int64_t slot = 2 * (int64_t)g + (g == g0 ? first_slot : 0);
     return k == a.d ? a.part_db[slot * kOwned + in_tile] : a.part[(slot * DP + k) * kOwned + in_tile];
   };
   auto wanted = [&](int k) { return k < a.d ? a.dW != nullptr : k == a.d && a.db != nullptr; };
@@ -1064,8 +1091,11 @@ __global__ __launch_bounds__(256) void head_list_kernel(const PrepareArgs a) {
     m.splits = __shfl(real, (int)(least & 63));
     m.tiles_per = __shfl(per, (int)(least & 63));
     m.row_steps = (at + kTile - 1) / kTile;
-    // runs of four steps at least
-    m.groups = (int32_t)min((int64_t)a.round, ((int64_t)(a.padded_classes / kOwned) * m.row_steps + 3) / 4);
+    // Equal runs (of four steps at least) where that is faster than whole class tiles in rounds: the shares of cut tiles take as long to write and
+    // to add up as about 24 steps.  517 rows x 50,021 classes (17 steps, 391 class tiles): 67 + 75 us in equal runs, 79 in whole tiles.
+    const int64_t class_tiles = a.padded_classes / kOwned, pairs = class_tiles * m.row_steps;
+    const int64_t whole = (class_tiles + a.round - 1) / a.round * (m.row_steps + 2), equal = pairs / a.round + 24;
+    m.groups = m.row_steps == 0 ? 0 : whole <= equal ? (int32_t)class_tiles : (int32_t)min((int64_t)a.round, (pairs + 3) / 4);
     if (lane == 0) *a.meta = m;
     // what stands behind the last labelled row, up to a whole workgroup's
     for (int i = at + lane; i < m.row_tiles * kOwned; i += 64) {
@@ -1235,7 +1265,7 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   k.db = c.db;
   k.part = reinterpret_cast<float *>(at(p.part_dW));
   k.part_db = reinterpret_cast<float *>(at(p.part_db));
-  const int64_t groups = std::min<int64_t>(round_of(p.DP), ((int64_t)p.class_tiles * ((rows + kTile - 1) / kTile) + 3) / 4);  // at most
+  const int64_t groups = std::max<int64_t>(round_of(p.DP), p.class_tiles);  // at most
   hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, (kAll < kClassesInRegs ? kAll : kClassesInRegs)>), dim3((unsigned)groups), dim3(256), 0, s, k);
   HEAD_TRY(hipGetLastError());
   // many shares of few class tiles: a workgroup per row of dW; few shares of many: some rows each
