@@ -408,23 +408,15 @@ def _room(name: str, workspace, device):
     return workspace.data_ptr(), workspace.numel()
 
 
-class _On:
-    """The call's device is the current one inside, and its current stream is the call's."""
-
-    def __init__(self, name: str, device):
-        import torch
-        if device.type != "cuda":
-            _refuse(name, f"tensors must be on a GPU, not on {device}")
-        self._guard = torch.cuda.device(device)
-        self._device = device
-
-    def __enter__(self):
-        import torch
-        self._guard.__enter__()
-        return C.c_void_p(torch.cuda.current_stream(self._device).cuda_stream)
-
-    def __exit__(self, *exc):
-        return self._guard.__exit__(*exc)
+def _launch(name: str, device, fn, *args) -> int:
+    """Calls ``fn`` with the current stream of the tensors' device, which is the current device meanwhile."""
+    import torch
+    if device.type != "cuda":
+        _refuse(name, f"tensors must be on a GPU, not on {device}")
+    if torch.cuda.current_device() == device.index:
+        return fn(*args, torch.cuda.current_stream().cuda_stream)
+    with torch.cuda.device(device):
+        return fn(*args, torch.cuda.current_stream().cuda_stream)
 
 
 def _stored(name: str, q, scale, device):
@@ -446,8 +438,7 @@ def gnnstage_rows8_store(x, q, scale) -> None:
     rows, d = x.shape
     if tuple(q.shape) != (rows, (d + 31) // 32 * 32):
         _refuse(name, f"q must have the shape {(rows, (d + 31) // 32 * 32)}, not {tuple(q.shape)}")
-    with _On(name, x.device) as stream:
-        rc = lib.gnnstage_rows8_store(x.data_ptr(), dt, ld_x, rows, d, q.data_ptr(), ld_q, scale.data_ptr(), ld_s, stream)
+    rc = _launch(name, x.device, lib.gnnstage_rows8_store, x.data_ptr(), dt, ld_x, rows, d, q.data_ptr(), ld_q, scale.data_ptr(), ld_s)
     if rc != 0:
         raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
 
@@ -461,8 +452,7 @@ def gnnstage_rows8_load(q, scale, x) -> None:
     rows, d = x.shape
     if tuple(q.shape) != (rows, (d + 31) // 32 * 32):
         _refuse(name, f"q must have the shape {(rows, (d + 31) // 32 * 32)}, not {tuple(q.shape)}")
-    with _On(name, x.device) as stream:
-        rc = lib.gnnstage_rows8_load(q.data_ptr(), ld_q, scale.data_ptr(), ld_s, rows, d, x.data_ptr(), dt, ld_x, stream)
+    rc = _launch(name, x.device, lib.gnnstage_rows8_load, q.data_ptr(), ld_q, scale.data_ptr(), ld_s, rows, d, x.data_ptr(), dt, ld_x)
     if rc != 0:
         raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
 
@@ -491,9 +481,8 @@ def gnnstage_rows8_weight_grad(q, scale, dY, dW, workspace, dbias=None) -> None:
     if dbias is not None:
         _tensor(name, "dbias", dbias, (d_out,), torch.float32, dev)
     ws, size = _room(name, workspace, dev)
-    with _On(name, dev) as stream:
-        rc = lib.gnnstage_rows8_weight_grad(q.data_ptr(), ld_q, scale.data_ptr(), ld_s, dY.data_ptr(), dt, ld_dy, q.shape[0], d, d_out,
-                                            dW.data_ptr(), None if dbias is None else dbias.data_ptr(), ws, size, stream)
+    rc = _launch(name, dev, lib.gnnstage_rows8_weight_grad, q.data_ptr(), ld_q, scale.data_ptr(), ld_s, dY.data_ptr(), dt, ld_dy, q.shape[0], d,
+                 d_out, dW.data_ptr(), None if dbias is None else dbias.data_ptr(), ws, size)
     if rc != 0:
         raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
 
@@ -747,9 +736,8 @@ def gnntrain_head_xent(h, W, bias, labels, mask, inv_n_train: float, row_loss, w
     ld_dh = d if dh is None else _matrix(name, "dh", dh, (rows, d), h.dtype, dev)
     ws, size = _room(name, workspace, dev)
     ptr = lambda t: None if t is None else t.data_ptr()
-    with _On(name, dev) as stream:
-        rc = lib.gnntrain_head_xent(h.data_ptr(), ld_h, W.data_ptr(), dt, ptr(bias), labels.data_ptr(), ptr(mask), rows, d, n_classes,
-                                    float(inv_n_train), row_loss.data_ptr(), ptr(dh), ld_dh, ptr(dW), ptr(db), ws, size, stream)
+    rc = _launch(name, dev, lib.gnntrain_head_xent, h.data_ptr(), ld_h, W.data_ptr(), dt, ptr(bias), labels.data_ptr(), ptr(mask), rows, d,
+                 n_classes, float(inv_n_train), row_loss.data_ptr(), ptr(dh), ld_dh, ptr(dW), ptr(db), ws, size)
     if rc != 0:
         raise GnnStageError(rc, lib.gnntrain_last_error(None).decode())
 

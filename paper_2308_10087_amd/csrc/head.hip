@@ -130,6 +130,36 @@ __global__ __launch_bounds__(256) void piece_grad_kernel(float *logits, int ld, 
   }
 }
 
+// Both at once where the classes are one piece: loss and gradients of a row.
+__global__ __launch_bounds__(256) void whole_grad_kernel(float *logits, int ld, const float *bias, const int32_t *label, int64_t rows, int n,
+                                                         float inv_n, float *row_loss, bf16_t *high, bf16_t *low) {
+  const int lane = threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= rows) return;
+  float *z = logits + (size_t)r * ld;
+  const int y = label[r];
+  const bool on = y >= 0;
+  float mx = -INFINITY, others = 0.f;
+  for (int c = lane; c < n; c += 64) mx = fmaxf(mx, z[c] + (bias ? bias[c] : 0.f));
+  mx = wave_max(mx);
+  for (int c = lane; c < n; c += 64)
+    if (c != y) others += expf(z[c] + (bias ? bias[c] : 0.f) - mx);
+  others = wave_sum(others);
+  const float zl = on ? z[y] + (bias ? bias[y] : 0.f) - mx : 0.f, own = expf(zl), sum = others + own, inv_sum = 1.f / sum;
+  for (int c = lane; c < ld; c += 64) {
+    float g = 0.f;
+    if (on && c < n) g = (c == y ? -others : expf(z[c] + (bias ? bias[c] : 0.f) - mx)) * inv_sum * inv_n;
+    if (high != nullptr) {
+      const bf16_t x = (bf16_t)g;
+      high[(size_t)r * ld + c] = x;
+      low[(size_t)r * ld + c] = (bf16_t)(g - (float)x);
+    } else {
+      z[c] = g;
+    }
+  }
+  if (lane == 0 && on) row_loss[r] = own > 0.5f * sum ? log1pf(others / own) : logf(sum) - zl;
+}
+
 // dh = what the pieces have added up, in the rows' type; zeros for rows without a label
 __global__ __launch_bounds__(256) void finish_rows_kernel(const float *acc, const int32_t *label, int64_t rows, int d, void *dh, int dtype,
                                                           int64_t ld_dh) {
@@ -229,7 +259,8 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
   auto at = [&](size_t off) { return c.ws + off; };
   const StageWeightsArgs w{c.W, p.d, p.C, at(p.Wt), p.Kp, at(p.Wn), p.Cp};
   HEAD_TRY(launch_stage_weights(&w, 1, p.dtype, nullptr, s));
-  if (p.grads) HEAD_TRY(launch_fill_zero(at(p.zeros), sizeof(float) * (size_t)round_up(p.d, 64), s));
+  const bool one = p.piece >= p.C;
+  if (c.dh && !one) HEAD_TRY(launch_fill_zero(at(p.zeros), sizeof(float) * (size_t)round_up(p.d, 64), s));
   float *logits = reinterpret_cast<float *>(at(p.logits)), *acc = reinterpret_cast<float *>(at(p.acc));
   int32_t *label = reinterpret_cast<int32_t *>(at(p.label));
   RowState *state = reinterpret_cast<RowState *>(at(p.state));
@@ -262,6 +293,11 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
     for (int c0 = 0; c0 < p.C; c0 += p.piece) {
       const int n = std::min(p.piece, p.C - c0);
       HEAD_TRY(piece_logits(c0, n));
+      if (one && p.grads) {
+        hipLaunchKernelGGL(whole_grad_kernel, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, n, c.inv_n, c.row_loss + row0, high, low);
+        HEAD_TRY(hipGetLastError());
+        continue;
+      }
       hipLaunchKernelGGL(piece_state_kernel, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, (int)(c0 + n == p.C), state,
                          c.row_loss + row0);
       HEAD_TRY(hipGetLastError());
@@ -269,9 +305,11 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
     if (!p.grads) continue;
     for (int c0 = 0; c0 < p.C; c0 += p.piece) {
       const int n = std::min(p.piece, p.C - c0);
-      if (p.piece < p.C) HEAD_TRY(piece_logits(c0, n));  // the only piece's are still there
-      hipLaunchKernelGGL(piece_grad_kernel, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low);
-      HEAD_TRY(hipGetLastError());
+      if (!one) {
+        HEAD_TRY(piece_logits(c0, n));
+        hipLaunchKernelGGL(piece_grad_kernel, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low);
+        HEAD_TRY(hipGetLastError());
+      }
       if (c.dh) {
         GemmNtArgs g{};
         g.A = high ? (const void *)high : logits;  // dh is of the rows' type: the rounding of its factors to bf16 is below its own
@@ -294,7 +332,7 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
         HEAD_TRY(launch_gemm_nt(g, p.dtype, s));
       }
       if (c.dW || c.db) {
-        const bool whole = p.piece >= p.C && c.dW;
+        const bool whole = one && c.dW;
         float *tmp = whole ? c.dW : reinterpret_cast<float *>(at(p.tmp));
         if (!whole) HEAD_TRY(launch_fill_zero(tmp, sizeof(float) * (size_t)p.d * n, s));
         for (int part = 0; part < (high ? 2 : 1); ++part) {
@@ -473,18 +511,18 @@ template <int DP>
 __device__ void fill_rows(const RowsArgs &a) {
   constexpr int per_row = DP / 8;
   const bool wide = (a.ld_dh & 7) == 0 && (reinterpret_cast<uintptr_t>(a.dh) & 15u) == 0;
-  const int64_t step = (int64_t)a.fills * 256, all = a.all_rows * per_row;
+  const int64_t all = a.all_rows * per_row;
   // (eight pieces' labels are asked for at a time: no read passes the writes in front of it)
-  for (int64_t i0 = ((int64_t)blockIdx.x - a.items) * 256 + threadIdx.x; i0 < all; i0 += 8 * step) {
+  for (int64_t i0 = ((int64_t)blockIdx.x - a.items) * 2048 + threadIdx.x; i0 < all; i0 += (int64_t)a.fills * 2048) {
     bool zero[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int64_t row = min(i0 + u * step, all - 1) / per_row;
+      const int64_t row = min(i0 + u * 256, all - 1) / per_row;
       zero[u] = (a.mask != nullptr && a.mask[row] == 0) | ((uint32_t)a.labels[row] >= (uint32_t)a.C);
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int64_t i = i0 + u * step;
+      const int64_t i = i0 + u * 256;
       const int k = (int)(i % per_row) * 8;
       if (i >= all || k >= a.d || !zero[u]) continue;
       bf16_t *dst = a.dh + (size_t)(i / per_row * a.ld_dh) + k;
@@ -1234,7 +1272,7 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   constexpr int kAll = DP / 16;
   const bool sums = c.dh != nullptr;
   r.items = (int32_t)std::min(row_tiles * p.max_splits, std::max<int64_t>(row_tiles, kRowItems));
-  r.fills = sums ? (int32_t)std::min<int64_t>(1024, (rows * (DP / 8) + 1023) / 1024) : 0;
+  r.fills = sums ? (int32_t)std::min<int64_t>(1024, (rows * (DP / 8) + 2047) / 2048) : 0;
   r.labels = c.labels;
   r.mask = c.mask;
   r.all_rows = rows;
