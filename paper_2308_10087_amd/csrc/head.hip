@@ -390,6 +390,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef bf16_t bf16x4 __attribute__((ext_vector_type(4)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896f;
 constexpr float kNoMax = -3.4028234663852886e38f;  // the least number: of a row that has seen no more than minus infinity
@@ -527,7 +528,8 @@ __device__ void fill_rows(const RowsArgs &a) {
       if (i >= all || k >= a.d || !zero[u]) continue;
       bf16_t *dst = a.dh + (size_t)(i / per_row * a.ld_dh) + k;
       if (wide && k + 8 <= a.d) {
-        *reinterpret_cast<bf16x8 *>(dst) = bf16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        // (past the caches: 179 MB of zeros went through them in 64 us, 28 so)
+        __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, reinterpret_cast<u32x4 *>(dst));
       } else {
 #pragma unroll
         for (int t = 0; t < 8; ++t)
@@ -704,7 +706,7 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
         if (to < 0) continue;
         bf16_t *dst = a.dh + (size_t)((int64_t)to * a.ld_dh) + c;
         if (wide && c + 8 <= a.d) {
-          *reinterpret_cast<bf16x8 *>(dst) = o;
+          __builtin_nontemporal_store(__builtin_bit_cast(u32x4, o), reinterpret_cast<u32x4 *>(dst));  // (41 classes: 156 us through the caches, 144 so)
         } else {
 #pragma unroll
           for (int t = 0; t < 8; ++t)
@@ -1208,8 +1210,10 @@ FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads) {
   return p;
 }
 
-// Owned operands in registers, of d / 16: all of them where the registers reach.
-constexpr int kRowsInRegs = 12, kClassesInRegs = 8;  // width 256
+// Owned operands in registers, of d / 16 (the others in LDS): as many as the registers reach for.  Width 256, 18 k rows x 100 k classes: rows kernel
+// 8 / 12 / 16 4.14 / 4.11 / 4.09 ms (all of them, then), classes kernel 4 / 8 / 12 4.59 / 4.11 / 4.10 ms.
+template <int DP>
+constexpr int kClassesInRegs = DP == 256 ? 10 : DP == 128 ? 6 : 4;
 
 // a slab of at most p.rows rows; first: the weights are not there yet
 template <int DP, bool DIRECT>
@@ -1272,11 +1276,11 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   constexpr int kAll = DP / 16;
   const bool sums = c.dh != nullptr;
   r.items = (int32_t)std::min(row_tiles * p.max_splits, std::max<int64_t>(row_tiles, kRowItems));
-  r.fills = sums ? (int32_t)std::min<int64_t>(1024, (rows * (DP / 8) + 2047) / 2048) : 0;
+  r.fills = sums ? (int32_t)std::min<int64_t>(8192, (rows * (DP / 8) + 2047) / 2048) : 0;
   r.labels = c.labels;
   r.mask = c.mask;
   r.all_rows = rows;
-  hipLaunchKernelGGL((sums ? head_rows_kernel<DP, true, DIRECT, (kAll < kRowsInRegs ? kAll : kRowsInRegs)> : head_rows_kernel<DP, false, DIRECT, kAll>),
+  hipLaunchKernelGGL((sums ? head_rows_kernel<DP, true, DIRECT, kAll> : head_rows_kernel<DP, false, DIRECT, kAll>),
                      dim3((unsigned)(r.items + r.fills)), dim3(256), 0, s, r);
   HEAD_TRY(hipGetLastError());
   if (p.max_splits > 1) {
@@ -1304,7 +1308,7 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   k.part = reinterpret_cast<float *>(at(p.part_dW));
   k.part_db = reinterpret_cast<float *>(at(p.part_db));
   const int64_t groups = std::max<int64_t>(round_of(p.DP), p.class_tiles);  // at most
-  hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, (kAll < kClassesInRegs ? kAll : kClassesInRegs)>), dim3((unsigned)groups), dim3(256), 0, s, k);
+  hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, kClassesInRegs<DP>>), dim3((unsigned)groups), dim3(256), 0, s, k);
   HEAD_TRY(hipGetLastError());
   // many shares of few class tiles: a workgroup per row of dW; few shares of many: some rows each
   const unsigned gy = p.class_tiles < 64 ? (unsigned)p.d + 1 : 8u;
