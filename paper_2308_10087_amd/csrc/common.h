@@ -441,6 +441,15 @@ int launch_ln_param_reduce(const LnReduceArgs *red, int n, hipStream_t s);
 // dst[r][c] = src[r][c] for c < d, zero for d <= c < dst_ld
 int launch_copy_rows(const void *src, int src_ld, void *dst, int dst_ld, int64_t M, int d, int dtype, hipStream_t s);
 
+// ---- fp32 products of the loss head (head32.hip) ---------------------------------------------------
+// C[M x N] (+)= A[M x K] . B[N x K]^T: 16-byte aligned rows, K a multiple of 4
+int launch_nt32(const float *A, int64_t lda, const float *B, int64_t ldb, int M, int N, int K, float *C, int64_t ldc, bool add, hipStream_t s);
+// D[I x O] += A[M x I]^T . B[M x O], sums[o] += column sums of B (D or sums may be NULL): 16-byte aligned rows, readable up to I and O rounded up to 4.
+// part: tn32_splits(M, I, O) * I * O floats (or max_splits as many), part_sum: the same times O
+int tn32_splits(int64_t M, int I, int O);
+int launch_tn32(const float *A, int64_t lda, const float *B, int64_t ldb, int M, int I, int O, float *D, int64_t ldd, float *sums, float *part,
+                float *part_sum, int max_splits, hipStream_t s);
+
 // ---- rows in 8 bits -----------------------------------------------------------------------------
 // q (16-byte aligned, ld_q a multiple of 16 and at least d rounded up to 32, written up to there) and scale (a byte per 32 columns) from
 // rows of any alignment

@@ -72,23 +72,55 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const void *h, int dtype
   }
 }
 
-// The classes [c0, c0 + n) of a slab's rows; a wave per row.
-__global__ __launch_bounds__(256) void piece_state_kernel(const float *logits, int ld, const float *bias, const int32_t *label, int64_t rows,
+// Rows of a piece's logits: a wave per row, four rows per workgroup, or (WAVES = 16) a workgroup per row where the classes are kWideRow or more, so that few
+// rows occupy more of the card and a lane's chain of exponentials is short.  100 x 50,021: 647 us with a wave per row, 46 with a workgroup.
+constexpr int kWideRow = 2048;
+
+template <int WAVES>
+constexpr int row_threads = WAVES == 1 ? 256 : 64 * WAVES;
+
+template <int WAVES>
+__device__ __forceinline__ int64_t my_row() {
+  return WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : (int64_t)blockIdx.x;
+}
+
+// over the lanes that share a row; every lane gets the result
+template <int WAVES, bool MAX>
+__device__ __forceinline__ float row_join(float v) {
+  v = MAX ? wave_max(v) : wave_sum(v);
+  if constexpr (WAVES > 1) {
+    __shared__ float part[WAVES];
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v = MAX ? fmaxf(v, part[w]) : v + part[w];
+  }
+  return v;
+}
+
+// The classes [c0, c0 + n) of a slab's rows.
+template <int WAVES>
+__global__ __launch_bounds__(row_threads<WAVES>) void piece_state_kernel(const float *logits, int ld, const float *bias, const int32_t *label, int64_t rows,
                                                           int c0, int n, int last, RowState *state, float *row_loss) {
-  const int lane = threadIdx.x & 63;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int kStep = 64 * WAVES;
+  const int lane = threadIdx.x & (kStep - 1);
+  const int64_t r = my_row<WAVES>();
   if (r >= rows) return;
   const int y = label[r] - c0;
   if (label[r] < 0) return;
   const float *z = logits + (size_t)r * ld;
   RowState s = state[r];
   float mx = s.max;
-  for (int c = lane; c < n; c += 64) mx = fmaxf(mx, z[c] + (bias ? bias[c0 + c] : 0.f));
-  mx = wave_max(mx);
+#pragma unroll 4
+  for (int c = lane; c < n; c += kStep) mx = fmaxf(mx, z[c] + (bias ? bias[c0 + c] : 0.f));
+  mx = row_join<WAVES, true>(mx);
   float others = 0.f;
-  for (int c = lane; c < n; c += 64)
+#pragma unroll 4
+  for (int c = lane; c < n; c += kStep)
     if (c != y) others += expf(z[c] + (bias ? bias[c0 + c] : 0.f) - mx);
-  others = wave_sum(others);
+  others = row_join<WAVES, false>(others);
   // nothing but logits of minus infinity so far: there is no sum yet (their differences are no numbers)
   if (mx == -INFINITY)
     others = 0.f;
@@ -107,17 +139,19 @@ __global__ __launch_bounds__(256) void piece_state_kernel(const float *logits, i
 
 // The gradients of a piece's logits: fp32 in place, or as the sum of two bf16 numbers (16 bits of significand: the weight
 // gradient is fp32 and keeps more than one bf16 number holds).  Columns [n, ld) are written as zeros.
-__global__ __launch_bounds__(256) void piece_grad_kernel(float *logits, int ld, const float *bias, const int32_t *label, int64_t rows, int c0,
+template <int WAVES>
+__global__ __launch_bounds__(row_threads<WAVES>) void piece_grad_kernel(float *logits, int ld, const float *bias, const int32_t *label, int64_t rows, int c0,
                                                          int n, float inv_n, const RowState *state, bf16_t *high, bf16_t *low) {
-  const int lane = threadIdx.x & 63;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int kStep = 64 * WAVES;
+  const int lane = threadIdx.x & (kStep - 1);
+  const int64_t r = my_row<WAVES>();
   if (r >= rows) return;
   float *z = logits + (size_t)r * ld;
   const bool on = label[r] >= 0;
   const int y = label[r] - c0;
   const RowState s = state[r];
   const float inv_sum = 1.f / (s.others + expf(s.own - s.max));
-  for (int c = lane; c < ld; c += 64) {
+  for (int c = lane; c < ld; c += kStep) {
     float g = 0.f;
     if (on && c < n) g = (c == y ? -s.others : expf(z[c] + (bias ? bias[c0 + c] : 0.f) - s.max)) * inv_sum * inv_n;
     if (high != nullptr) {
@@ -131,22 +165,27 @@ __global__ __launch_bounds__(256) void piece_grad_kernel(float *logits, int ld, 
 }
 
 // Both at once where the classes are one piece: loss and gradients of a row.
-__global__ __launch_bounds__(256) void whole_grad_kernel(float *logits, int ld, const float *bias, const int32_t *label, int64_t rows, int n,
+template <int WAVES>
+__global__ __launch_bounds__(row_threads<WAVES>) void whole_grad_kernel(float *logits, int ld, const float *bias, const int32_t *label, int64_t rows, int n,
                                                          float inv_n, float *row_loss, bf16_t *high, bf16_t *low) {
-  const int lane = threadIdx.x & 63;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int kStep = 64 * WAVES;
+  const int lane = threadIdx.x & (kStep - 1);
+  const int64_t r = my_row<WAVES>();
   if (r >= rows) return;
   float *z = logits + (size_t)r * ld;
   const int y = label[r];
   const bool on = y >= 0;
+  const float zy = on ? z[y] + (bias ? bias[y] : 0.f) : 0.f;  // read before the joins below: in fp32 the gradients overwrite it
   float mx = -INFINITY, others = 0.f;
-  for (int c = lane; c < n; c += 64) mx = fmaxf(mx, z[c] + (bias ? bias[c] : 0.f));
-  mx = wave_max(mx);
-  for (int c = lane; c < n; c += 64)
+#pragma unroll 4
+  for (int c = lane; c < n; c += kStep) mx = fmaxf(mx, z[c] + (bias ? bias[c] : 0.f));
+  mx = row_join<WAVES, true>(mx);
+#pragma unroll 4
+  for (int c = lane; c < n; c += kStep)
     if (c != y) others += expf(z[c] + (bias ? bias[c] : 0.f) - mx);
-  others = wave_sum(others);
-  const float zl = on ? z[y] + (bias ? bias[y] : 0.f) - mx : 0.f, own = expf(zl), sum = others + own, inv_sum = 1.f / sum;
-  for (int c = lane; c < ld; c += 64) {
+  others = row_join<WAVES, false>(others);
+  const float zl = on ? zy - mx : 0.f, own = expf(zl), sum = others + own, inv_sum = 1.f / sum;
+  for (int c = lane; c < ld; c += kStep) {
     float g = 0.f;
     if (on && c < n) g = (c == y ? -others : expf(z[c] + (bias ? bias[c] : 0.f) - mx)) * inv_sum * inv_n;
     if (high != nullptr) {
@@ -169,6 +208,20 @@ __global__ __launch_bounds__(256) void finish_rows_kernel(const float *acc, cons
   store_elt(dh, dtype, (size_t)(r * ld_dh + i % d), label[r] >= 0 ? acc[i] : 0.f);
 }
 
+// out[c][r] = in[r][c], r < rows, c < n: 32 x 32 at a time
+template <typename T>
+__global__ __launch_bounds__(256) void turn_kernel(const T *in, int64_t ld, int rows, int n, T *out, int64_t ld_out) {
+  __shared__ T tile[32][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c0 = blockIdx.x * 32, r0 = blockIdx.y * 32;
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    if (r0 + y + i < rows && c0 + x < n) tile[y + i][x] = in[(size_t)(r0 + y + i) * ld + c0 + x];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    if (c0 + y + i < n && r0 + x < rows) out[(size_t)(c0 + y + i) * ld_out + r0 + x] = tile[x][y + i];
+}
+
 // dW[k][c0 + c] += piece[k][c], c < n
 __global__ __launch_bounds__(256) void add_piece_kernel(const float *piece, int d, int n, float *dW, int C, int c0) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -176,21 +229,34 @@ __global__ __launch_bounds__(256) void add_piece_kernel(const float *piece, int 
   dW[(size_t)(i / n) * C + c0 + i % n] += piece[i];
 }
 
-constexpr int kPieceClasses = 8192;
+constexpr int kPieceClasses = 8192;  // at least, where rows are many; few rows' logits are one piece
 constexpr int64_t kPieceElements = 1 << 26;  // logits of a slab's piece
 constexpr int64_t kSlabRows = 131072;
 
+// Which fp32 products serve.  rows x width x classes, in us, on the products of the stages' layers / on the head's own (head32.hip, tiles of 128 rows):
+// 2,000 x 256 x 1,000 85 / 112, 34,493 x 256 x 172 209 / 278, 34,493 x 256 x 1,000 733 / 742, 100,000 x 64 x 1,000 901 / 1,176;
+// 5,000 x 500 x 1,500 364 / 333, 5,000 x 1,000 x 700 332 / 295, 5,196 x 1,000 x 2,003 840 / 725.
+constexpr int kOwnWidth = 384;
+constexpr double kOwnWork = 3e9;  // rows * classes * width
+// Few rows against many classes: dh = g W^T is a sum over the classes with few outputs, which the products above give to as few workgroups.  With the gradients
+// turned it is one over the rows of its operands, which is cut into many.  rows x width x classes, fp32, in us, as they are / turned: 100 x 256 x 50,021 686 / 359,
+// 2,000 x 128 x 20,000 1,414 / 851; 1,000 x 600 x 2,000 169 / 174, 4,096 x 256 x 4,096 367 / 383, 300 x 64 x 800 46 / 55.
+constexpr int64_t kFewRows = 4096;
+constexpr int kManyClasses = 8192;
 struct Plan {
   int64_t rows = 0, slab = 0;
-  int d = 0, C = 0, dtype = 0, elt = 4, Kp = 0, Cp = 0, piece = 0, ld = 0, max_splits = 0;
+  int d = 0, C = 0, dtype = 0, elt = 4, Kp = 0, Cp = 0, piece = 0, ld = 0, max_splits = 0, max_splits_turned = 0;
   bool grads = false;
-  size_t Wt = 0, Wn = 0, rows_at = 0, label = 0, state = 0, logits = 0, high = 0, low = 0, acc = 0, zeros = 0, tmp = 0, partial = 0,
+  bool own32 = false;   // fp32 products on the head's own kernels
+  bool turned = false;  // dh from the turned gradients
+  int ld_turned = 0;
+  size_t Wt = 0, Wn = 0, rows_at = 0, label = 0, state = 0, logits = 0, high = 0, low = 0, acc = 0, zeros = 0, tmp = 0, turn = 0, partial = 0,
          bias_partial = 0, total = 0;
 };
 
 bool make_plan(int64_t rows, int d, int C, int dtype, bool grads, Plan &p, std::string &err) {
   if (rows < 0 || rows > ((int64_t)1 << 40)) { err = "rows must not be negative (nor beyond 2^40)"; return false; }
-  if (d < 1 || d > 65536) { err = "the rows' width must be in [1, 65536]"; return false; }
+  if (d < 1 || d > 65534) { err = "the rows' width must be in [1, 65534]"; return false; }
   if (C < 1 || C > (1 << 24)) { err = "n_classes must be in [1, 2^24]"; return false; }
   if (dtype != GNNSTAGE_F32 && dtype != GNNSTAGE_BF16) { err = "unknown dtype"; return false; }
   p.rows = rows;
@@ -201,12 +267,16 @@ bool make_plan(int64_t rows, int d, int C, int dtype, bool grads, Plan &p, std::
   p.grads = grads;
   p.Kp = round_up(d, 8);
   p.Cp = round_up(C, 8);
-  p.piece = std::min(p.Cp, kPieceClasses);
+  const int64_t few = std::max<int64_t>(1, std::min(rows, kSlabRows));
+  p.piece = (int)std::min<int64_t>(p.Cp, std::max<int64_t>(kPieceClasses, kPieceElements / 2 / std::max<int64_t>(few, d) / 8 * 8));
   p.ld = p.piece;
   p.slab = std::max<int64_t>(128, std::min(kSlabRows, kPieceElements / std::max(p.ld, p.d)));
   p.slab = std::min(p.slab, std::max<int64_t>(rows, 1));
-  const int tiles = (d + 127) / 128 * ((p.piece + 127) / 128);
-  p.max_splits = std::max(1, std::min(256, 1024 / tiles));
+  const int64_t tiles = (int64_t)((d + 127) / 128) * ((p.piece + 127) / 128);
+  p.turned = grads && p.slab <= kFewRows && C >= kManyClasses;
+  p.own32 = dtype == GNNSTAGE_F32 && !p.turned && d >= kOwnWidth && (double)p.slab * C * d >= kOwnWork;
+  p.ld_turned = round_up((int)p.slab, 8);
+  p.max_splits = p.own32 ? tn32_splits(p.slab, d, p.piece) : (int)std::max<int64_t>(1, std::min<int64_t>(256, 1024 / tiles));
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -214,6 +284,8 @@ bool make_plan(int64_t rows, int d, int C, int dtype, bool grads, Plan &p, std::
     return at;
   };
   const size_t m = (size_t)p.slab;
+  // as many as the room for the weight gradients' partial sums holds
+  p.max_splits_turned = (int)std::max<int64_t>(1, std::min<int64_t>(256, (int64_t)p.max_splits * std::max<int64_t>(p.piece, p.slab) / p.slab));
   p.Wt = take((size_t)p.elt * C * p.Kp);
   p.Wn = take((size_t)p.elt * d * p.Cp);
   p.rows_at = take((size_t)p.elt * m * p.Kp);
@@ -224,9 +296,10 @@ bool make_plan(int64_t rows, int d, int C, int dtype, bool grads, Plan &p, std::
     p.high = take(dtype == GNNSTAGE_BF16 ? 2 * m * p.ld : 0);
     p.low = take(dtype == GNNSTAGE_BF16 ? 2 * m * p.ld : 0);
     p.acc = take(sizeof(float) * m * d);
-    p.zeros = take(sizeof(float) * (size_t)round_up(d, 64));
-    p.tmp = take(sizeof(float) * (size_t)d * p.piece);
-    p.partial = take(sizeof(float) * (size_t)p.max_splits * d * p.piece);
+    p.zeros = take(p.own32 ? 0 : sizeof(float) * (size_t)round_up(d, 64));
+    p.tmp = take(p.own32 ? 0 : sizeof(float) * (size_t)d * p.piece);
+    p.turn = take(p.turned ? (size_t)p.elt * p.piece * p.ld_turned : 0);
+    p.partial = take(sizeof(float) * (size_t)p.max_splits * d * std::max<size_t>(p.piece, p.turned ? m : 0));
     p.bias_partial = take(sizeof(float) * (size_t)p.max_splits * p.piece);
   }
   p.total = off;
@@ -259,8 +332,8 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
   auto at = [&](size_t off) { return c.ws + off; };
   const StageWeightsArgs w{c.W, p.d, p.C, at(p.Wt), p.Kp, at(p.Wn), p.Cp};
   HEAD_TRY(launch_stage_weights(&w, 1, p.dtype, nullptr, s));
-  const bool one = p.piece >= p.C;
-  if (c.dh && !one) HEAD_TRY(launch_fill_zero(at(p.zeros), sizeof(float) * (size_t)round_up(p.d, 64), s));
+  const bool one = p.piece >= p.C, own32 = p.own32;
+  if (c.dh && !one && !own32 && !p.turned) HEAD_TRY(launch_fill_zero(at(p.zeros), sizeof(float) * (size_t)round_up(p.d, 64), s));
   float *logits = reinterpret_cast<float *>(at(p.logits)), *acc = reinterpret_cast<float *>(at(p.acc));
   int32_t *label = reinterpret_cast<int32_t *>(at(p.label));
   RowState *state = reinterpret_cast<RowState *>(at(p.state));
@@ -269,11 +342,15 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
   for (int64_t row0 = 0; row0 < p.rows; row0 += p.slab) {
     const int64_t M = std::min(p.slab, p.rows - row0);
     const unsigned waves = (unsigned)((M + 3) / 4);
+    const bool wide = p.piece >= kWideRow;
     hipLaunchKernelGGL(pack_rows_kernel, dim3(waves), dim3(256), 0, s, static_cast<const char *>(c.h) + (size_t)(row0 * c.ld_h) * p.elt, p.dtype,
                        c.ld_h, c.labels + row0, c.mask ? c.mask + row0 : nullptr, M, p.d, p.C, (void *)at(p.rows_at), p.Kp, label, state,
                        c.row_loss + row0);
     HEAD_TRY(hipGetLastError());
     auto piece_logits = [&](int c0, int n) {
+      if (own32)
+        return launch_nt32(reinterpret_cast<const float *>(at(p.rows_at)), p.Kp, reinterpret_cast<const float *>(at(p.Wt)) + (size_t)c0 * p.Kp, p.Kp, (int)M,
+                           n, p.Kp, logits, p.ld, false, s);
       GemmNtArgs g{};
       g.A = at(p.rows_at);
       g.a_dtype = p.dtype;
@@ -294,12 +371,19 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
       const int n = std::min(p.piece, p.C - c0);
       HEAD_TRY(piece_logits(c0, n));
       if (one && p.grads) {
-        hipLaunchKernelGGL(whole_grad_kernel, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, n, c.inv_n, c.row_loss + row0, high, low);
+        if (wide)
+          hipLaunchKernelGGL(whole_grad_kernel<16>, dim3((unsigned)M), dim3(1024), 0, s, logits, p.ld, c.bias, label, M, n, c.inv_n, c.row_loss + row0, high, low);
+        else
+          hipLaunchKernelGGL(whole_grad_kernel<1>, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, n, c.inv_n, c.row_loss + row0, high, low);
         HEAD_TRY(hipGetLastError());
         continue;
       }
-      hipLaunchKernelGGL(piece_state_kernel, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, (int)(c0 + n == p.C), state,
-                         c.row_loss + row0);
+      if (wide)
+        hipLaunchKernelGGL(piece_state_kernel<16>, dim3((unsigned)M), dim3(1024), 0, s, logits, p.ld, c.bias, label, M, c0, n, (int)(c0 + n == p.C),
+                           state, c.row_loss + row0);
+      else
+        hipLaunchKernelGGL(piece_state_kernel<1>, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, (int)(c0 + n == p.C), state,
+                           c.row_loss + row0);
       HEAD_TRY(hipGetLastError());
     }
     if (!p.grads) continue;
@@ -307,10 +391,44 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
       const int n = std::min(p.piece, p.C - c0);
       if (!one) {
         HEAD_TRY(piece_logits(c0, n));
-        hipLaunchKernelGGL(piece_grad_kernel, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low);
+        if (wide)
+          hipLaunchKernelGGL(piece_grad_kernel<16>, dim3((unsigned)M), dim3(1024), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low);
+        else
+          hipLaunchKernelGGL(piece_grad_kernel<1>, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low);
         HEAD_TRY(hipGetLastError());
       }
-      if (c.dh) {
+      if (own32) {  // (columns of the gradients from n up to a multiple of 8 are zeros, and so are the weights')
+        if (c.dh)
+          HEAD_TRY(launch_nt32(logits, p.ld, reinterpret_cast<const float *>(at(p.Wn)) + c0, p.Cp, (int)M, p.d, round_up(n, 8), acc, p.d, c0 > 0, s));
+        if (c.dW || c.db)
+          HEAD_TRY(launch_tn32(reinterpret_cast<const float *>(at(p.rows_at)), p.Kp, logits, p.ld, (int)M, p.d, n, c.dW ? c.dW + c0 : nullptr, p.C,
+                               c.db ? c.db + c0 : nullptr, reinterpret_cast<float *>(at(p.partial)), reinterpret_cast<float *>(at(p.bias_partial)),
+                               p.max_splits, s));
+        continue;
+      }
+      if (c.dh && p.turned) {
+        if (c0 == 0) HEAD_TRY(launch_fill_zero(acc, sizeof(float) * (size_t)M * p.d, s));
+        const dim3 grid((unsigned)((n + 31) / 32), (unsigned)((M + 31) / 32));
+        if (high)
+          hipLaunchKernelGGL(turn_kernel<bf16_t>, grid, dim3(256), 0, s, high, p.ld, (int)M, n, reinterpret_cast<bf16_t *>(at(p.turn)), p.ld_turned);
+        else
+          hipLaunchKernelGGL(turn_kernel<float>, grid, dim3(256), 0, s, logits, p.ld, (int)M, n, reinterpret_cast<float *>(at(p.turn)), p.ld_turned);
+        HEAD_TRY(hipGetLastError());
+        GemmTnArgs t{};
+        t.A = at(p.turn);
+        t.a_dtype = p.dtype;
+        t.lda = p.ld_turned;
+        t.B = at(p.Wt) + (size_t)c0 * p.Kp * p.elt;
+        t.ldb = p.Kp;
+        t.M = n;
+        t.I = (int)M;
+        t.O = p.d;
+        t.scale = 1.f;
+        t.dW = acc;
+        t.partial = reinterpret_cast<float *>(at(p.partial));
+        t.max_splits = p.max_splits_turned;
+        HEAD_TRY(launch_gemm_tn(t, p.dtype, s));
+      } else if (c.dh) {
         GemmNtArgs g{};
         g.A = high ? (const void *)high : logits;  // dh is of the rows' type: the rounding of its factors to bf16 is below its own
         g.a_dtype = p.dtype;
