@@ -137,11 +137,11 @@ __global__ __launch_bounds__(row_threads<WAVES>) void piece_state_kernel(const f
   }
 }
 
-// The gradients of a piece's logits: fp32 in place, or as the sum of two bf16 numbers (16 bits of significand: the weight
-// gradient is fp32 and keeps more than one bf16 number holds).  Columns [n, ld) are written as zeros.
+// The gradients of a piece's logits: fp32 in place, or as the sum of three bf16 numbers, which is all of their bits: the weight
+// gradient is fp32.  Columns [n, ld) are written as zeros.
 template <int WAVES>
 __global__ __launch_bounds__(row_threads<WAVES>) void piece_grad_kernel(float *logits, int ld, const float *bias, const int32_t *label, int64_t rows, int c0,
-                                                         int n, float inv_n, const RowState *state, bf16_t *high, bf16_t *low) {
+                                                         int n, float inv_n, const RowState *state, bf16_t *high, bf16_t *low, bf16_t *lowest) {
   constexpr int kStep = 64 * WAVES;
   const int lane = threadIdx.x & (kStep - 1);
   const int64_t r = my_row<WAVES>();
@@ -156,8 +156,11 @@ __global__ __launch_bounds__(row_threads<WAVES>) void piece_grad_kernel(float *l
     if (on && c < n) g = (c == y ? -s.others : expf(z[c] + (bias ? bias[c0 + c] : 0.f) - s.max)) * inv_sum * inv_n;
     if (high != nullptr) {
       const bf16_t x = (bf16_t)g;
+      const float rest = g - (float)x;
+      const bf16_t y2 = (bf16_t)rest;
       high[(size_t)r * ld + c] = x;
-      low[(size_t)r * ld + c] = (bf16_t)(g - (float)x);
+      low[(size_t)r * ld + c] = y2;
+      lowest[(size_t)r * ld + c] = (bf16_t)(rest - (float)y2);
     } else {
       z[c] = g;
     }
@@ -167,7 +170,7 @@ __global__ __launch_bounds__(row_threads<WAVES>) void piece_grad_kernel(float *l
 // Both at once where the classes are one piece: loss and gradients of a row.
 template <int WAVES>
 __global__ __launch_bounds__(row_threads<WAVES>) void whole_grad_kernel(float *logits, int ld, const float *bias, const int32_t *label, int64_t rows, int n,
-                                                         float inv_n, float *row_loss, bf16_t *high, bf16_t *low) {
+                                                         float inv_n, float *row_loss, bf16_t *high, bf16_t *low, bf16_t *lowest) {
   constexpr int kStep = 64 * WAVES;
   const int lane = threadIdx.x & (kStep - 1);
   const int64_t r = my_row<WAVES>();
@@ -190,8 +193,11 @@ __global__ __launch_bounds__(row_threads<WAVES>) void whole_grad_kernel(float *l
     if (on && c < n) g = (c == y ? -others : expf(z[c] + (bias ? bias[c] : 0.f) - mx)) * inv_sum * inv_n;
     if (high != nullptr) {
       const bf16_t x = (bf16_t)g;
+      const float rest = g - (float)x;
+      const bf16_t y2 = (bf16_t)rest;
       high[(size_t)r * ld + c] = x;
-      low[(size_t)r * ld + c] = (bf16_t)(g - (float)x);
+      low[(size_t)r * ld + c] = y2;
+      lowest[(size_t)r * ld + c] = (bf16_t)(rest - (float)y2);
     } else {
       z[c] = g;
     }
@@ -250,7 +256,7 @@ struct Plan {
   bool own32 = false;   // fp32 products on the head's own kernels
   bool turned = false;  // dh from the turned gradients
   int ld_turned = 0;
-  size_t Wt = 0, Wn = 0, rows_at = 0, label = 0, state = 0, logits = 0, high = 0, low = 0, acc = 0, zeros = 0, tmp = 0, turn = 0, partial = 0,
+  size_t Wt = 0, Wn = 0, rows_at = 0, label = 0, state = 0, logits = 0, high = 0, low = 0, lowest = 0, acc = 0, zeros = 0, tmp = 0, turn = 0, partial = 0,
          bias_partial = 0, total = 0;
 };
 
@@ -295,6 +301,7 @@ bool make_plan(int64_t rows, int d, int C, int dtype, bool grads, Plan &p, std::
   if (grads) {
     p.high = take(dtype == GNNSTAGE_BF16 ? 2 * m * p.ld : 0);
     p.low = take(dtype == GNNSTAGE_BF16 ? 2 * m * p.ld : 0);
+    p.lowest = take(dtype == GNNSTAGE_BF16 ? 2 * m * p.ld : 0);
     p.acc = take(sizeof(float) * m * d);
     p.zeros = take(p.own32 ? 0 : sizeof(float) * (size_t)round_up(d, 64));
     p.tmp = take(p.own32 ? 0 : sizeof(float) * (size_t)d * p.piece);
@@ -339,6 +346,7 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
   RowState *state = reinterpret_cast<RowState *>(at(p.state));
   bf16_t *high = p.dtype == GNNSTAGE_BF16 ? reinterpret_cast<bf16_t *>(at(p.high)) : nullptr;
   bf16_t *low = p.dtype == GNNSTAGE_BF16 ? reinterpret_cast<bf16_t *>(at(p.low)) : nullptr;
+  bf16_t *lowest = p.dtype == GNNSTAGE_BF16 ? reinterpret_cast<bf16_t *>(at(p.lowest)) : nullptr;
   for (int64_t row0 = 0; row0 < p.rows; row0 += p.slab) {
     const int64_t M = std::min(p.slab, p.rows - row0);
     const unsigned waves = (unsigned)((M + 3) / 4);
@@ -372,9 +380,9 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
       HEAD_TRY(piece_logits(c0, n));
       if (one && p.grads) {
         if (wide)
-          hipLaunchKernelGGL(whole_grad_kernel<16>, dim3((unsigned)M), dim3(1024), 0, s, logits, p.ld, c.bias, label, M, n, c.inv_n, c.row_loss + row0, high, low);
+          hipLaunchKernelGGL(whole_grad_kernel<16>, dim3((unsigned)M), dim3(1024), 0, s, logits, p.ld, c.bias, label, M, n, c.inv_n, c.row_loss + row0, high, low, lowest);
         else
-          hipLaunchKernelGGL(whole_grad_kernel<1>, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, n, c.inv_n, c.row_loss + row0, high, low);
+          hipLaunchKernelGGL(whole_grad_kernel<1>, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, n, c.inv_n, c.row_loss + row0, high, low, lowest);
         HEAD_TRY(hipGetLastError());
         continue;
       }
@@ -392,9 +400,9 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
       if (!one) {
         HEAD_TRY(piece_logits(c0, n));
         if (wide)
-          hipLaunchKernelGGL(piece_grad_kernel<16>, dim3((unsigned)M), dim3(1024), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low);
+          hipLaunchKernelGGL(piece_grad_kernel<16>, dim3((unsigned)M), dim3(1024), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low, lowest);
         else
-          hipLaunchKernelGGL(piece_grad_kernel<1>, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low);
+          hipLaunchKernelGGL(piece_grad_kernel<1>, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low, lowest);
         HEAD_TRY(hipGetLastError());
       }
       if (own32) {  // (columns of the gradients from n up to a multiple of 8 are zeros, and so are the weights')
@@ -453,12 +461,12 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
         const bool whole = one && c.dW;
         float *tmp = whole ? c.dW : reinterpret_cast<float *>(at(p.tmp));
         if (!whole) HEAD_TRY(launch_fill_zero(tmp, sizeof(float) * (size_t)p.d * n, s));
-        for (int part = 0; part < (high ? 2 : 1); ++part) {
+        for (int part = 0; part < (high ? 3 : 1); ++part) {
           GemmTnArgs t{};
           t.A = at(p.rows_at);
           t.a_dtype = p.dtype;
           t.lda = p.Kp;
-          t.B = high ? (const void *)(part ? low : high) : logits;
+          t.B = high ? (const void *)(part == 0 ? high : part == 1 ? low : lowest) : logits;
           t.ldb = p.ld;
           t.M = (int)M;
           t.I = p.d;
@@ -511,6 +519,8 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896f;
+constexpr float kExactFrom = 1.f / 64;  // (1 / 2 takes as long)
+constexpr int kExactRows = 16384;
 constexpr float kNoMax = -3.4028234663852886e38f;  // the least number: of a row that has seen no more than minus infinity
 // exp(z - m): the difference first, so that it is exact for the logits that count, however large they are
 __device__ __forceinline__ float exp_diff(float z, float m) { return __builtin_amdgcn_exp2f((z - m) * kLog2e); }
@@ -926,7 +936,12 @@ struct ClassesArgs {
 // its run begins in that tile and in its second if it does not.
 __device__ inline int64_t run_begin(int64_t total, int groups, int g) { return total * g / groups; }
 
-template <int DP, bool DIRECT, int IN_REGS>
+//
+// EXACT: g with all of their bits.  16 bits are 2e-6 of a single term of dW; of a sum over many rows that is less than the rounding of the sum in fp32, over few rows
+// it is not.  So where the labelled rows are kExactRows at most, the tiles with large g (a label's, a sure row's: what a column of dW consists of, and in few
+// tiles where the classes are many) go around once more for the third bf16 number.  Relative error of dW, 16 bits / all: 370 rows of 96 classes 1.6e-6 / 2.3e-7,
+// 517 of 50,021 4.5e-7 / 2.4e-7 (183 / 190 us); 18,000 of 100,003 1.0e-6 / 9.8e-7 (4.0 / 4.2 ms), where fp32 products have 1.7e-6.
+template <int DP, bool DIRECT, bool EXACT, int IN_REGS>
 __global__ __launch_bounds__(256, kPerUnit<DP>) void head_classes_kernel(const ClassesArgs a) {
   typedef Geometry<DP> G;
   typedef Owned<DP, IN_REGS> Own;
@@ -943,7 +958,7 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_classes_kernel(const C
   __shared__ __attribute__((aligned(16))) char shared[Own::in_lds > 0 ? 4 * Own::in_lds * 1024 : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int row_steps = a.meta->row_steps, groups = a.meta->groups, n = a.meta->n, group = blockIdx.x;
-  if (group >= groups) return;
+  if (group >= groups || EXACT != (n <= kExactRows)) return;
   const int64_t total = (int64_t)a.class_tiles * row_steps, run0 = run_begin(total, groups, group), run1 = run_begin(total, groups, group + 1);
   Places<DP> at(wave, lane);
   int32_t index[DIRECT ? G::loads : 1];  // of the rows that this lane loads next
@@ -990,49 +1005,71 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_classes_kernel(const C
         look_up(tile + 2);
       }
       if (idle) return;
-      at.renew();
-      // (the bias first, as in the rows kernel: the same logits to the last bit, so that large ones meet their own maximum)
-      f32x16 z;
+      // Once, and where EXACT once more for the last bits of tiles that have large g: they are made again, since keeping them takes registers that are not there.
+      bool again = false;
+#pragma unroll 1
+      for (;;) {
+        at.renew();
+        // (the bias first, as in the rows kernel: the same logits to the last bit, so that large ones meet their own maximum)
+        f32x16 z;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) z[i] = bias;
+        for (int i = 0; i < 16; ++i) z[i] = bias;
 #pragma unroll
-      for (int ks = 0; ks < DP / 16; ++ks) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(first_operand<DP>(now, at.first, ks), own(ks), z, 0, 0, 0);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 m = *reinterpret_cast<const f32x4 *>(st->max + 8 * q + 4 * h), l = *reinterpret_cast<const f32x4 *>(st->log + 8 * q + 4 * h);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) z[4 * q + r] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + r] - m[r], kLog2e, l[r]));
-      }
-      if (__any((uint32_t)(st->label[lane & 31] - first) < 32u)) {
+        for (int ks = 0; ks < DP / 16; ++ks) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(first_operand<DP>(now, at.first, ks), own(ks), z, 0, 0, 0);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const i32x4 y = *reinterpret_cast<const i32x4 *>(st->label + 8 * q + 4 * h);
-          const f32x4 t = *reinterpret_cast<const f32x4 *>(st->t + 8 * q + 4 * h);
+          const f32x4 m = *reinterpret_cast<const f32x4 *>(st->max + 8 * q + 4 * h), l = *reinterpret_cast<const f32x4 *>(st->log + 8 * q + 4 * h);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) z[4 * q + r] = y[r] == c ? -t[r] : z[4 * q + r];
+          for (int r = 0; r < 4; ++r) z[4 * q + r] = __builtin_amdgcn_exp2f(fmaf(z[4 * q + r] - m[r], kLog2e, l[r]));
         }
-      }
-      // db takes g as it is; its long sum is compensated
-      float part = 0.f;
+        if (__any((uint32_t)(st->label[lane & 31] - first) < 32u)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) part += z[i];
-      const float y = part - g_low, s = g_sum + y;
-      g_low = (s - g_sum) - y;
-      g_sum = s;
-      bf16x8 high[2], low[2];  // g = high + low to 16 bits
+          for (int q = 0; q < 4; ++q) {
+            const i32x4 y = *reinterpret_cast<const i32x4 *>(st->label + 8 * q + 4 * h);
+            const f32x4 t = *reinterpret_cast<const f32x4 *>(st->t + 8 * q + 4 * h);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        high[i >> 3][i & 7] = (bf16_t)z[i];
-        low[i >> 3][i & 7] = (bf16_t)(z[i] - (float)high[i >> 3][i & 7]);
-      }
-#pragma unroll
-      for (int dt = 0; dt < DP / 32; ++dt)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const bf16x8 x = lds_turned<DP>(now, at.second, dt, t);
-          sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, high[t], sum[dt], 0, 0, 0);
-          sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, low[t], sum[dt], 0, 0, 0);
+            for (int r = 0; r < 4; ++r) z[4 * q + r] = y[r] == c ? -t[r] : z[4 * q + r];
+          }
         }
+        float largest = 0.f;
+        if (!again) {
+          // db takes g as it is; its long sum is compensated
+          float part = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            part += z[i];
+            if constexpr (EXACT) largest = fmaxf(largest, fabsf(z[i]));
+          }
+          const float y = part - g_low, s = g_sum + y;
+          g_low = (s - g_sum) - y;
+          g_sum = s;
+        }
+        const bool more = EXACT && __any(largest > kExactFrom);
+        bf16x8 high[2], low[2];  // g = high + low to 16 bits, + a third to all of them
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          high[i >> 3][i & 7] = (bf16_t)z[i];
+          z[i] -= (float)high[i >> 3][i & 7];
+          low[i >> 3][i & 7] = (bf16_t)z[i];
+        }
+        if (again) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            high[i >> 3][i & 7] = (bf16_t)(z[i] - (float)low[i >> 3][i & 7]);
+            low[i >> 3][i & 7] = (bf16_t)0.f;
+          }
+        }
+#pragma unroll
+        for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const bf16x8 x = lds_turned<DP>(now, at.second, dt, t);
+            sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, high[t], sum[dt], 0, 0, 0);
+            sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, low[t], sum[dt], 0, 0, 0);
+          }
+        if (!more) break;
+        again = true;
+      }
     };
     for (int tile = begin; tile < end; tile += 2) {
       step(tile, (const lds_char *)tile0, &stats0, (lds_char *)tile1, &stats1);
@@ -1426,8 +1463,12 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   k.part = reinterpret_cast<float *>(at(p.part_dW));
   k.part_db = reinterpret_cast<float *>(at(p.part_db));
   const int64_t groups = std::max<int64_t>(round_of(p.DP), p.class_tiles);  // at most
-  hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, kClassesInRegs<DP>>), dim3((unsigned)groups), dim3(256), 0, s, k);
+  hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, true, kClassesInRegs<DP>>), dim3((unsigned)groups), dim3(256), 0, s, k);
   HEAD_TRY(hipGetLastError());
+  if (rows > kExactRows) {  // how many have labels is known to the device: one of the two returns at once
+    hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, false, kClassesInRegs<DP>>), dim3((unsigned)groups), dim3(256), 0, s, k);
+    HEAD_TRY(hipGetLastError());
+  }
   // many shares of few class tiles: a workgroup per row of dW; few shares of many: some rows each
   const unsigned gy = p.class_tiles < 64 ? (unsigned)p.d + 1 : 8u;
   hipLaunchKernelGGL(head_reduce_kernel<DP>, dim3(2u * (unsigned)p.class_tiles, gy), dim3(256), 0, s, k);
