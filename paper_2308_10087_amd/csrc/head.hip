@@ -347,22 +347,27 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
   bf16_t *high = p.dtype == GNNSTAGE_BF16 ? reinterpret_cast<bf16_t *>(at(p.high)) : nullptr;
   bf16_t *low = p.dtype == GNNSTAGE_BF16 ? reinterpret_cast<bf16_t *>(at(p.low)) : nullptr;
   bf16_t *lowest = p.dtype == GNNSTAGE_BF16 ? reinterpret_cast<bf16_t *>(at(p.lowest)) : nullptr;
+  // Without gradients, rows in whole 16-byte pieces are read where they are: those without a label, which may hold anything, meet no other row.
+  // (450,061 x 600 x 103 classes, fp32: 1,681 us from a packed copy, 1,067 without.)
+  const bool in_place = !p.grads && p.d % 8 == 0 && c.ld_h * p.elt % 16 == 0 && (reinterpret_cast<uintptr_t>(c.h) & 15u) == 0 && c.ld_h <= INT32_MAX;
   for (int64_t row0 = 0; row0 < p.rows; row0 += p.slab) {
     const int64_t M = std::min(p.slab, p.rows - row0);
+    const char *h = static_cast<const char *>(c.h) + (size_t)(row0 * c.ld_h) * p.elt;
+    const char *rows_at = in_place ? h : at(p.rows_at);
+    const int64_t ld_rows = in_place ? c.ld_h : p.Kp;
     const unsigned waves = (unsigned)((M + 3) / 4);
     const bool wide = p.piece >= kWideRow;
-    hipLaunchKernelGGL(pack_rows_kernel, dim3(waves), dim3(256), 0, s, static_cast<const char *>(c.h) + (size_t)(row0 * c.ld_h) * p.elt, p.dtype,
-                       c.ld_h, c.labels + row0, c.mask ? c.mask + row0 : nullptr, M, p.d, p.C, (void *)at(p.rows_at), p.Kp, label, state,
-                       c.row_loss + row0);
+    hipLaunchKernelGGL(pack_rows_kernel, dim3(waves), dim3(256), 0, s, h, p.dtype, c.ld_h, c.labels + row0, c.mask ? c.mask + row0 : nullptr, M, p.d, p.C,
+                       (void *)at(p.rows_at), in_place ? 0 : p.Kp, label, state, c.row_loss + row0);
     HEAD_TRY(hipGetLastError());
     auto piece_logits = [&](int c0, int n) {
       if (own32)
-        return launch_nt32(reinterpret_cast<const float *>(at(p.rows_at)), p.Kp, reinterpret_cast<const float *>(at(p.Wt)) + (size_t)c0 * p.Kp, p.Kp, (int)M,
+        return launch_nt32(reinterpret_cast<const float *>(rows_at), ld_rows, reinterpret_cast<const float *>(at(p.Wt)) + (size_t)c0 * p.Kp, p.Kp, (int)M,
                            n, p.Kp, logits, p.ld, false, s);
       GemmNtArgs g{};
-      g.A = at(p.rows_at);
+      g.A = rows_at;
       g.a_dtype = p.dtype;
-      g.lda = p.Kp;
+      g.lda = ld_rows;
       g.Bt = at(p.Wt) + (size_t)c0 * p.Kp * p.elt;
       g.ldb = p.Kp;
       g.M = (int)M;

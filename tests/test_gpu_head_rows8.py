@@ -174,6 +174,18 @@ def test_masked_rows_may_hold_anything(rows, d, C, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,C,pad", [(300, 64, 41, 0), (300, 64, 41, 8), (300, 64, 41, 1), (260, 512, 70, 0), (260, 512, 70, 8), (140001, 392, 30, 0), (90, 33, 8200, 7)])
+def test_losses_alone_beside_masked_rows_of_anything(rows, d, C, pad, dtype):
+    h, W, b, y, mask = head_inputs(rows, d, C, dtype, 17, "some")
+    on = counts(y, mask, C)
+    h[~torch.from_numpy(on)] = float("nan")
+    want, mag = head_formula(h.double().numpy(), W.double().numpy(), b.astype(np.float64), y, on, 1.0)
+    got = run_head(h, W, b, y, mask, 1.0, dtype, grads=(), pad=pad)["loss"]
+    assert np.all(np.abs(got - want["loss"]) <= head_bounds(want, mag, d, C, int(on.sum()), dtype)["loss"])
+    assert np.all(got[~on] == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("lowest", [-float("inf"), -3.4028234663852886e38])
 def test_classes_left_out_by_their_bias(dtype, lowest):
     """Left out first, last, in whole runs longer than any tile; none of the rows' own."""
