@@ -274,13 +274,13 @@ bool make_plan(int64_t rows, int d, int C, int dtype, bool grads, Plan &p, std::
   p.Kp = round_up(d, 8);
   p.Cp = round_up(C, 8);
   const int64_t few = std::max<int64_t>(1, std::min(rows, kSlabRows));
-  p.piece = (int)std::min<int64_t>(p.Cp, std::max<int64_t>(kPieceClasses, kPieceElements / 2 / std::max<int64_t>(few, d) / 8 * 8));
+  p.piece = (int)std::min<int64_t>(p.Cp, std::max<int64_t>(kPieceClasses, kPieceElements / std::max<int64_t>(few, d) / 8 * 8));
   p.ld = p.piece;
   p.slab = std::max<int64_t>(128, std::min(kSlabRows, kPieceElements / std::max(p.ld, p.d)));
   p.slab = std::min(p.slab, std::max<int64_t>(rows, 1));
   const int64_t tiles = (int64_t)((d + 127) / 128) * ((p.piece + 127) / 128);
   p.turned = grads && p.slab <= kFewRows && C >= kManyClasses;
-  p.own32 = dtype == GNNSTAGE_F32 && !p.turned && d >= kOwnWidth && (double)p.slab * C * d >= kOwnWork;
+  p.own32 = dtype == GNNSTAGE_F32 && d >= kOwnWidth && (double)p.slab * C * d >= kOwnWork;
   p.ld_turned = round_up((int)p.slab, 8);
   p.max_splits = p.own32 ? tn32_splits(p.slab, d, p.piece) : (int)std::max<int64_t>(1, std::min<int64_t>(256, 1024 / tiles));
   size_t off = 0;
@@ -410,15 +410,6 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
           hipLaunchKernelGGL(piece_grad_kernel<1>, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low, lowest);
         HEAD_TRY(hipGetLastError());
       }
-      if (own32) {  // (columns of the gradients from n up to a multiple of 8 are zeros, and so are the weights')
-        if (c.dh)
-          HEAD_TRY(launch_nt32(logits, p.ld, reinterpret_cast<const float *>(at(p.Wn)) + c0, p.Cp, (int)M, p.d, round_up(n, 8), acc, p.d, c0 > 0, s));
-        if (c.dW || c.db)
-          HEAD_TRY(launch_tn32(reinterpret_cast<const float *>(at(p.rows_at)), p.Kp, logits, p.ld, (int)M, p.d, n, c.dW ? c.dW + c0 : nullptr, p.C,
-                               c.db ? c.db + c0 : nullptr, reinterpret_cast<float *>(at(p.partial)), reinterpret_cast<float *>(at(p.bias_partial)),
-                               p.max_splits, s));
-        continue;
-      }
       if (c.dh && p.turned) {
         if (c0 == 0) HEAD_TRY(launch_fill_zero(acc, sizeof(float) * (size_t)M * p.d, s));
         const dim3 grid((unsigned)((n + 31) / 32), (unsigned)((M + 31) / 32));
@@ -427,21 +418,36 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
         else
           hipLaunchKernelGGL(turn_kernel<float>, grid, dim3(256), 0, s, logits, p.ld, (int)M, n, reinterpret_cast<float *>(at(p.turn)), p.ld_turned);
         HEAD_TRY(hipGetLastError());
-        GemmTnArgs t{};
-        t.A = at(p.turn);
-        t.a_dtype = p.dtype;
-        t.lda = p.ld_turned;
-        t.B = at(p.Wt) + (size_t)c0 * p.Kp * p.elt;
-        t.ldb = p.Kp;
-        t.M = n;
-        t.I = (int)M;
-        t.O = p.d;
-        t.scale = 1.f;
-        t.dW = acc;
-        t.partial = reinterpret_cast<float *>(at(p.partial));
-        t.max_splits = p.max_splits_turned;
-        HEAD_TRY(launch_gemm_tn(t, p.dtype, s));
-      } else if (c.dh) {
+        if (own32) {
+          HEAD_TRY(launch_tn32(reinterpret_cast<const float *>(at(p.turn)), p.ld_turned, reinterpret_cast<const float *>(at(p.Wt)) + (size_t)c0 * p.Kp, p.Kp, n,
+                               (int)M, p.d, acc, p.d, nullptr, reinterpret_cast<float *>(at(p.partial)), nullptr, p.max_splits_turned, s));
+        } else {
+          GemmTnArgs t{};
+          t.A = at(p.turn);
+          t.a_dtype = p.dtype;
+          t.lda = p.ld_turned;
+          t.B = at(p.Wt) + (size_t)c0 * p.Kp * p.elt;
+          t.ldb = p.Kp;
+          t.M = n;
+          t.I = (int)M;
+          t.O = p.d;
+          t.scale = 1.f;
+          t.dW = acc;
+          t.partial = reinterpret_cast<float *>(at(p.partial));
+          t.max_splits = p.max_splits_turned;
+          HEAD_TRY(launch_gemm_tn(t, p.dtype, s));
+        }
+      }
+      if (own32) {  // (columns of the gradients from n up to a multiple of 8 are zeros, and so are the weights')
+        if (c.dh && !p.turned)
+          HEAD_TRY(launch_nt32(logits, p.ld, reinterpret_cast<const float *>(at(p.Wn)) + c0, p.Cp, (int)M, p.d, round_up(n, 8), acc, p.d, c0 > 0, s));
+        if (c.dW || c.db)
+          HEAD_TRY(launch_tn32(reinterpret_cast<const float *>(at(p.rows_at)), p.Kp, logits, p.ld, (int)M, p.d, n, c.dW ? c.dW + c0 : nullptr, p.C,
+                               c.db ? c.db + c0 : nullptr, reinterpret_cast<float *>(at(p.partial)), reinterpret_cast<float *>(at(p.bias_partial)),
+                               p.max_splits, s));
+        continue;
+      }
+      if (c.dh && !p.turned) {
         GemmNtArgs g{};
         g.A = high ? (const void *)high : logits;  // dh is of the rows' type: the rounding of its factors to bf16 is below its own
         g.a_dtype = p.dtype;
