@@ -72,8 +72,10 @@ __global__ __launch_bounds__(256) void pack_rows_kernel(const void *h, int dtype
   }
 }
 
-// Rows of a piece's logits: a wave per row, four rows per workgroup, or (WAVES = 16) a workgroup per row where the classes are kWideRow or more, so that few
-// rows occupy more of the card and a lane's chain of exponentials is short.  100 x 50,021: 647 us with a wave per row, 46 with a workgroup.
+// Rows of a piece's logits: a wave per row, four rows per workgroup, or (WAVES = 16) a workgroup per row where the classes are many, so that few rows occupy
+// more of the card and a lane's chain of exponentials is short: from 2,048 classes on where the rows are few, else from 4,096.  The kernel alone, 100 x 50,021:
+// 647 us with a wave per row, 46 with a workgroup; calls of width 64 in fp32, waves / workgroups: 1,000 x 600 49 / 51, 1,000 x 2,100 78 / 69, 5,000 x 2,100
+// 138 / 148, 20,000 x 2,100 377 / 447, 5,000 x 8,000 399 / 373, 20,000 x 8,000 1,584 / 1,415.
 constexpr int kWideRow = 2048;
 
 template <int WAVES>
@@ -264,6 +266,7 @@ bool make_plan(int64_t rows, int d, int C, int dtype, bool grads, Plan &p, std::
   if (rows < 0 || rows > ((int64_t)1 << 40)) { err = "rows must not be negative (nor beyond 2^40)"; return false; }
   if (d < 1 || d > 65534) { err = "the rows' width must be in [1, 65534]"; return false; }
   if (C < 1 || C > (1 << 24)) { err = "n_classes must be in [1, 2^24]"; return false; }
+  if ((int64_t)C * d > (int64_t)1 << 33) { err = "the weights must be 2^33 elements at most"; return false; }  // (a launch lays them out, 2^32 threads at most)
   if (dtype != GNNSTAGE_F32 && dtype != GNNSTAGE_BF16) { err = "unknown dtype"; return false; }
   p.rows = rows;
   p.d = d;
@@ -356,7 +359,7 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
     const char *rows_at = in_place ? h : at(p.rows_at);
     const int64_t ld_rows = in_place ? c.ld_h : p.Kp;
     const unsigned waves = (unsigned)((M + 3) / 4);
-    const bool wide = p.piece >= kWideRow;
+    const bool wide = p.piece >= (M <= kFewRows ? kWideRow : 2 * kWideRow);
     hipLaunchKernelGGL(pack_rows_kernel, dim3(waves), dim3(256), 0, s, h, p.dtype, c.ld_h, c.labels + row0, c.mask ? c.mask + row0 : nullptr, M, p.d, p.C,
                        (void *)at(p.rows_at), in_place ? 0 : p.Kp, label, state, c.row_loss + row0);
     HEAD_TRY(hipGetLastError());
@@ -520,7 +523,7 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
 // direct-to-LDS path, serves both products.
 // Bound by the matrix cores: per owned and streamed vector 4 d operations (rows kernel), 6 d (classes kernel: g enters as the sum
 // of two bf16 numbers, since dW is fp32), per wave and tile 32 (48) matrix instructions at d = 256 and half the LDS bandwidth.
-// Two workgroups of four waves per compute unit: one's exponentials run under the other's products.
+// Two workgroups of four waves per compute unit at width 256 (three at 128, four at 64): one's exponentials run under the other's products.
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -1519,6 +1522,7 @@ extern "C" int gnntrain_head_xent(const void *h, int64_t ld_h, const void *W, in
   if (ld_h < d || (dh != nullptr && ld_dh < d)) return train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: a leading dimension is below d");
   if (rows == 0) return GNNSTAGE_OK;
   if (!h || !W || !labels || !row_loss) return train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: h, W, labels and row_loss must not be NULL");
+  if (dh == h) return train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: dh must not be h, which is read after dh is written");
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: workspace must be 256-byte aligned");
   if (workspace_bytes < workspace_bytes_of(p)) return train_error(GNNSTAGE_ENOMEM, "gnntrain_head_xent: workspace smaller than gnntrain_head_xent_workspace_size()");
   const Call c{h, ld_h, W, bias, labels, mask, inv_n_train, row_loss, dh, ld_dh, dW, db, static_cast<char *>(workspace)};

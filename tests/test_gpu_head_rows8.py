@@ -157,6 +157,37 @@ def test_head_over_many_rows(rows, d, C, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_most_classes(dtype):
+    """2^24 of them (the formula on the GPU, in 64 bits).  The softmax's sum over 2^24 terms is one of partial sums of 2^17 at most."""
+    g = _g()
+    rows, d, C = 3, 4, 1 << 24
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    W = torch.randn(d, C, device=DEV, generator=gen).to(DT[dtype])
+    h = torch.randn(rows, d, device=DEV, generator=gen).to(DT[dtype])
+    y = torch.tensor([0, C - 1, 12345678], dtype=torch.int32, device=DEV)
+    loss, dh = torch.empty(rows, device=DEV), torch.empty_like(h)
+    dW, db = torch.zeros(d, C, device=DEV), torch.zeros(C, device=DEV)
+    ws = torch.empty(g.gnntrain_head_xent_workspace_size(rows, d, C, _code(g, dtype)), dtype=torch.uint8, device=DEV)
+    g.gnntrain_head_xent(h, W, None, y, None, 1.0, loss, ws, dh=dh, dW=dW, db=db)
+    z = h.double() @ W.double()
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    want = (lse - z.gather(1, y.long().unsqueeze(1))).squeeze(1)
+    p = torch.exp(z - lse)
+    p[torch.arange(rows, device=DEV), y.long()] -= 1.0
+    rel = 2 * 2 ** 17 * U  # of the softmax: its sum's, and what the logits' own roundings come to beside that
+    assert float((loss.double() - want).abs().max()) <= rel + 1e-5
+    assert float((db.double() - p.sum(0)).abs().max()) <= rel + 1e-6
+    big = p.abs().sum(0)
+    assert bool(((db.double() - p.sum(0)).abs() <= (rel + 8 * U + V * V) * big + 1e-30).all())
+    for k in range(d):
+        terms = h[:, k].double().unsqueeze(1) * p
+        assert bool(((dW[k].double() - terms.sum(0)).abs() <= (rel + 8 * U + V * V) * terms.abs().sum(0) + 1e-30).all())
+    dh_mag = p.abs() @ W.double().abs().t().contiguous()
+    dh_want = p @ W.double().t().contiguous()
+    assert bool(((dh.double() - dh_want).abs() <= (rel + (2 * V if dtype == "bf16" else 0)) * dh_mag + V * dh_want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,d,C", [(3011, 520, 2003), (2900, 397, 2741), (1500, 300, 9001), (1299, 390, 8999), (8400, 392, 8300)])
 def test_head_of_wide_rows_over_many_classes(rows, d, C, dtype):
     """Wide products; classes in more than one piece, for the last one of rows in more than one as well."""

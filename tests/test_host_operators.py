@@ -22,7 +22,8 @@ def _head(h=AT, ld_h=64, W=AT, dtype=1, bias=None, labels=AT, mask=None, rows=10
                                       (dict(n_classes=(1 << 24) + 1), -1), (dict(dtype=2), -1), (dict(dtype=-1), -1), (dict(ld_h=63), -1),
                                       (dict(dh=AT, ld_dh=63), -1), (dict(h=None), -1), (dict(W=None), -1), (dict(labels=None), -1),
                                       (dict(row_loss=None), -1), (dict(ws=None), -1), (dict(ws=AT + 16), -1), (dict(size=0), -4),
-                                      (dict(dW=AT, size=1000), -4)])
+                                      (dict(dW=AT, size=1000), -4), (dict(dh=AT), -1), (dict(d=65535), -1),
+                                      (dict(d=1024, ld_h=1024, n_classes=1 << 24), -1)])
 def test_head_refuses(bad, code):
     assert _head(**bad) == code
     assert "gnntrain_head_xent" in lib.gnntrain_last_error(None).decode()
