@@ -412,6 +412,44 @@ def test_head_on_another_stream_and_in_a_graph():
                 assert torch.equal(a, e), (dtype, rows, turn)
 
 
+@pytest.mark.parametrize("dtype,rows,d,C", [("f32", 1299, 390, 8999), ("bf16", 200, 300, 9000), ("f32", 3011, 520, 2003), ("bf16", 20000, 128, 172), ("bf16", 20000, 40, 300),
+                                            ("bf16", 1, 256, 20011)])
+def test_replays_and_calls_at_once(dtype, rows, d, C):
+    """A graph whose replays find few labelled rows, all, none; two streams at work at the same time, each with a workspace of its own."""
+    g = _g()
+    size = g.gnntrain_head_xent_workspace_size(rows, d, C, _code(g, dtype))
+    h, W, b, y, _ = head_inputs(rows, d, C, dtype, 31, "all")
+    inputs = [x.to(DEV) for x in (h, W, torch.from_numpy(b), torch.from_numpy(y))] + [torch.ones(rows, dtype=torch.uint8, device=DEV)]
+
+    def outputs():
+        return (torch.empty(rows, device=DEV), torch.empty(rows, d, dtype=DT[dtype], device=DEV), torch.zeros(d, C, device=DEV), torch.zeros(C, device=DEV),
+                torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV))
+
+    def call(out):
+        out[2].zero_()
+        out[3].zero_()
+        g.gnntrain_head_xent(*inputs, 0.01, out[0], out[4], dh=out[1], dW=out[2], db=out[3])
+
+    first, second, want = outputs(), outputs(), outputs()
+    call(first)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(first)
+    side = torch.cuda.Stream()
+    for share in (1.0, 0.1, 0.0, 0.95, 1.0):
+        inputs[4].copy_((torch.rand(rows, generator=torch.Generator().manual_seed(7)) < share).to(torch.uint8))
+        call(want)
+        torch.cuda.synchronize()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call(second)
+        graph.replay()
+        torch.cuda.synchronize()
+        for out in (first, second):
+            assert all(torch.equal(x, e) for x, e in zip(out[:4], want[:4])), share
+
+
 # ---- rows in 8 bits ------------------------------------------------------------------------------------------------
 def stored(x):
     """q, scale and the values they stand for, of float64 rows, from the definition."""
