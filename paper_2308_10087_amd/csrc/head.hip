@@ -535,6 +535,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.44269504088896f;
 constexpr float kExactFrom = 1.f / 64;  // (1 / 2 takes as long)
 constexpr int kExactRows = 16384;
+constexpr float kCoarseTo = 1.f / 32;  // see mean_scale
 constexpr float kNoMax = -3.4028234663852886e38f;  // the least number: of a row that has seen no more than minus infinity
 // exp(z - m): the difference first, so that it is exact for the logits that count, however large they are
 __device__ __forceinline__ float exp_diff(float z, float m) { return __builtin_amdgcn_exp2f((z - m) * kLog2e); }
@@ -642,7 +643,7 @@ struct RowsArgs {
   int64_t ld_dh;
   float *max, *log, *t;     // of the labelled rows: the row's maximum, -log2 of its sum, o / l
   float *part;              // [item][wave][DP][32]: sum p W
-  float *part_stat;         // [item][3][kOwned]: maximum, others, the label's logit
+  float *part_stat;         // [item][4][kOwned]: maximum, others, the label's logit, the sum of the factors that part was made with
   // workgroups from items on write the zeros of the other rows' dh: memory's work, next to the matrix cores'
   int32_t items, fills;
   const int32_t *labels;    // by row
@@ -683,16 +684,40 @@ __device__ void fill_rows(const RowsArgs &a) {
 
 // The end of a row, from its maximum, the others' sum and the label's logit.
 struct RowEnd {
-  float inv, t, loss, log;
+  float t, loss, log;
 };
 __device__ inline RowEnd end_row(float m, float others, float zl) {
   const float y = zl - m, own = exp_diff(zl, m), sum = others + own;
   RowEnd e;
-  e.inv = 1.f / sum;
   e.t = others / sum;
   e.loss = own > 0.5f * sum ? log1pf(others / own) : logf(sum) - y;
   e.log = -log2f(sum);  // (apart from the maximum, which may be so large that a sum of the two has lost it)
   return e;
+}
+
+// dh = inv_n t (sum_c p W_c / sum_c p - W_y), t = o / l: the mean of the other classes' weights less the label's.  What all classes' weights have in common is in
+// both and has to cancel, so the mean's factors p are added up as the product takes them, rounded (held), not as they were.  A factor of one bf16 number is
+// then off by 2^-8 of itself times its weights' distance from the mean; tiles with a factor above kCoarseTo of what the row has added up so far go around once
+// more with what the first number has left (2^-16).  The factors that stay coarse cost at most 1.6e-3 sqrt(kCoarseTo) = 2.9e-4 of dh beside its own rounding's 1.65e-3.
+// Relative error of dh, 2,000 rows of 256 columns, 41 classes whose weights share a column of 0 / 4 / 16 times what tells them apart: 1.69 / 2.03 / 4.82e-3 with
+// coarse factors against the sum of the unrounded ones, 1.66e-3 throughout so; it differs from fp32 factors' by 3e-5 to 8e-5 (before 1e-3 to 5e-3).
+// Calls in us with coarse factors / kCoarseTo 1/32 / 1/64 / 1/256: 46,657 x 100 x 10,007 (half labelled) 364 / 389 / 403 / 427, 517 x 256 x 50,021 170 / 180 / 184 / 187,
+// 20,011 x 256 x 100,003 3,990 / 4,050 / 4,080 / 4,275, 232,965 x 256 x 41 132 / 135 / 135 / 135.
+__device__ inline float mean_scale(float t, float held) { return held > 0.f ? t / held : 0.f; }
+
+typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+// the sum of a lane's 16 factors
+__device__ __forceinline__ float sum_of(const bf16x8 (&p)[2]) {
+  const bf16x2 one = {(bf16_t)1.f, (bf16_t)1.f};
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p[i], p[i], 0, 1), one, s, false);
+    s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p[i], p[i], 2, 3), one, s, false);
+    s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p[i], p[i], 4, 5), one, s, false);
+    s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(p[i], p[i], 6, 7), one, s, false);
+  }
+  return s;
 }
 
 template <int DP, bool GRAD, bool DIRECT, int IN_REGS>
@@ -716,7 +741,7 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
   // (past the last labelled row: that row once more, whatever it gives is not written)
   f32x16 sum[DP / 32];
   clear<DP>(sum);
-  float m = kNoMax, others = 0.f, zl = -INFINITY;
+  float m = kNoMax, others = 0.f, zl = -INFINITY, held = 0.f;
   Places<DP> at(wave, lane);
   const int tiles = (a.C + kTile - 1) / kTile, begin = split * meta.tiles_per, end = min(tiles, begin + meta.tiles_per);
   auto load = [&](int tile, lds_char *dst, float *bias) {
@@ -750,6 +775,7 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
       m = up;
       others *= f;
       if constexpr (GRAD) {
+        held *= f;
 #pragma unroll
         for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
@@ -764,22 +790,36 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
           zl = z[i];
           z[i] = -INFINITY;
         }
+      most = z[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) most = fmaxf(most, z[i]);
     }
-    bf16x8 p[2];
     float part = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float x = exp_diff(z[i], m);
-      part += x;
-      p[i >> 3][i & 7] = (bf16_t)x;  // dh is bf16: the rounding of a factor is no more than its own
+      z[i] = exp_diff(z[i], m);
+      part += z[i];
     }
     others += part;
     if constexpr (GRAD) {
+      // once, and where factors are large once more for what the first number has left of them
+      bool again = __any(exp_diff(most, m) > kCoarseTo * others);
+#pragma unroll 1
+      for (;;) {
+        bf16x8 p[2];
 #pragma unroll
-      for (int dt = 0; dt < DP / 32; ++dt)
+        for (int i = 0; i < 16; ++i) p[i >> 3][i & 7] = (bf16_t)z[i];
+        held += sum_of(p);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_turned<DP>(now, at.second, dt, t), p[t], sum[dt], 0, 0, 0);
+        for (int dt = 0; dt < DP / 32; ++dt)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            sum[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_turned<DP>(now, at.second, dt, t), p[t], sum[dt], 0, 0, 0);
+        if (!again) break;
+        again = false;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] -= (float)p[i >> 3][i & 7];
+      }
     }
   };
   for (int tile = begin; tile < end; tile += 2) {
@@ -787,14 +827,16 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
     if (tile + 1 < end) step(tile + 1, (const lds_char *)tile1, bias1, (lds_char *)tile0, bias0);
   }
   others += __shfl_xor(others, 32);
+  if constexpr (GRAD) held += __shfl_xor(held, 32);
   zl = __shfl(zl, (lane & 31) + 32 * ((label >> 2) & 1));  // from the half that had the label
   const int i = first + (lane & 31);
   if (splits > 1) {
-    float *stat = a.part_stat + (size_t)item * 3 * kOwned + wave * 32 + (lane & 31);
+    float *stat = a.part_stat + (size_t)item * 4 * kOwned + wave * 32 + (lane & 31);
     if (h == 0) {
       stat[0] = m;
       stat[kOwned] = others;
       stat[2 * kOwned] = zl;
+      if constexpr (GRAD) stat[3 * kOwned] = held;
     }
     if constexpr (GRAD) {
       float *out = a.part + ((size_t)item * 4 + wave) * DP * 32 + (lane & 31);
@@ -815,6 +857,7 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
     a.t[i] = e.t;
   }
   if constexpr (GRAD) {
+    const float scale = mean_scale(e.t, held);
     // A lane has four columns side by side of its row at a time; through LDS (the tiles are done with) a row's pieces come together: half of
     // the columns in a pass, 16-byte pieces permuted by the row.
     const bf16_t *wy = a.W + (size_t)max(label, 0) * DP;
@@ -835,7 +878,7 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_rows_kernel(const Rows
         for (int q = 0; q < 4; ++q) {
           bf16x4 o;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[r] = (bf16_t)((sum[pass * (DP / 64) + dt][4 * q + r] * e.inv - e.t * (float)w[dt][q][r]) * a.inv_n);
+          for (int r = 0; r < 4; ++r) o[r] = (bf16_t)((sum[pass * (DP / 64) + dt][4 * q + r] * scale - e.t * (float)w[dt][q][r]) * a.inv_n);
           const int piece = 4 * dt + q, at_row = lane & 31;
           *reinterpret_cast<LDS_AS bf16x4 *>(room + at_row * DP + ((piece ^ (at_row & (pieces - 1))) << 4) + 8 * h) = o;
         }
@@ -867,19 +910,20 @@ __global__ __launch_bounds__(256) void head_join_kernel(const RowsArgs a) {
   const Meta &meta = *a.meta;
   const int splits = meta.splits, row_tile = blockIdx.x >> 2, wave = blockIdx.x & 3, d0 = blockIdx.y * kJoinColumns;
   if (splits == 1 || row_tile >= meta.row_tiles) return;
-  __shared__ float stat[3][kMaxSplits][32], red[8][32];
+  __shared__ float stat[GRAD ? 4 : 3][kMaxSplits][32], red[8][32];
   __shared__ float turned[32][kJoinColumns + 1];
-  __shared__ float inv[32], ts[32];
+  __shared__ float scale[32], ts[32];
   __shared__ int label[32], row[32];
   const int n = threadIdx.x & 31, g = threadIdx.x >> 5, i = row_tile * kOwned + wave * 32 + n;
   const int64_t item0 = (int64_t)row_tile * splits;
   const int lab = a.label[i];
   float m = kNoMax;
   for (int s = g; s < splits; s += 8) {
-    const float *p = a.part_stat + (size_t)(item0 + s) * 3 * kOwned + wave * 32 + n;
+    const float *p = a.part_stat + (size_t)(item0 + s) * 4 * kOwned + wave * 32 + n;
     stat[0][s][n] = p[0];
     stat[1][s][n] = p[kOwned];
     stat[2][s][n] = p[2 * kOwned];
+    if constexpr (GRAD) stat[3][s][n] = p[3 * kOwned];
     m = fmaxf(m, p[0]);
   }
   red[g][n] = m;
@@ -894,12 +938,15 @@ __global__ __launch_bounds__(256) void head_join_kernel(const RowsArgs a) {
   }
   __syncthreads();
   if (g == 0) {
-    float others = 0.f;
-    for (int s = 0; s < splits; ++s) others += stat[1][s][n];
+    float others = 0.f, held = 0.f;
+    for (int s = 0; s < splits; ++s) {
+      others += stat[1][s][n];
+      if constexpr (GRAD) held += stat[0][s][n] * stat[3][s][n];
+    }
     const float zl = lab >= 0 ? stat[2][lab / kTile / meta.tiles_per][n] : -INFINITY;
     const RowEnd e = end_row(m, others, zl);
     const bool on = i < meta.n;
-    inv[n] = e.inv;
+    scale[n] = mean_scale(e.t, held);
     ts[n] = e.t;
     label[n] = on ? lab : -1;
     row[n] = on ? a.list[i] : -1;
@@ -926,7 +973,7 @@ __global__ __launch_bounds__(256) void head_join_kernel(const RowsArgs a) {
     const int r = k / kJoinColumns, c = k % kJoinColumns;
     if (label[r] >= 0 && d0 + c < a.d)
       a.dh[(size_t)((int64_t)row[r] * a.ld_dh) + d0 + c] =
-          (bf16_t)((turned[r][c] * inv[r] - ts[r] * (float)a.W[(size_t)label[r] * DP + d0 + c]) * a.inv_n);
+          (bf16_t)((turned[r][c] * scale[r] - ts[r] * (float)a.W[(size_t)label[r] * DP + d0 + c]) * a.inv_n);
   }
 }
 
@@ -1370,7 +1417,7 @@ FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads) {
   p.Wt = take(2 * (size_t)p.padded_classes * p.DP);
   p.bias = take(sizeof(float) * (size_t)p.padded_classes);
   const int64_t part_items = p.max_splits > 1 ? std::min<int64_t>(p.max_items, kRowItems) : 0;
-  p.part_stat = take(sizeof(float) * 3 * kOwned * (size_t)part_items);
+  p.part_stat = take(sizeof(float) * 4 * kOwned * (size_t)part_items);
   p.part = take(grads ? sizeof(float) * (size_t)kOwned * p.DP * (size_t)part_items : 0);
   const int64_t groups = grads ? std::min<int64_t>(round_of(p.DP), ((int64_t)p.class_tiles * ((rows + kTile - 1) / kTile) + 3) / 4) : 0;
   p.part_dW = take(sizeof(float) * 2 * (size_t)groups * p.DP * kOwned);

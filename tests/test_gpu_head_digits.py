@@ -1,0 +1,84 @@
+"""How many digits the gradients of the loss head without logits (gnntrain_head_xent) have, where its other tests' bounds leave room for fewer.
+
+u = 2^-24 is half a step of fp32 relative to the value, v = 2^-8 of bf16, so v^2 what the sum of two bf16 numbers leaves out."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_head_rows8 import DT, U, V, counts, head_formula, run_head
+
+pytestmark = pytest.mark.gpu
+
+COARSE = 2.0 ** -5  # a probability up to this share of its row's sum may enter dh as one bf16 number
+
+
+def leaning(rows, d, C, dtype, seed, common, lean=2.0):
+    """Rows that lean towards their class.  Of the columns in which they are zero, which logits do not see, the classes' weights share one ``common`` times as
+    large as what tells them apart."""
+    rng = np.random.default_rng(seed)
+    seen = (d + 1) // 2
+    W = rng.normal(size=(d, C)) / np.sqrt(seen)
+    y = rng.integers(0, C, size=rows).astype(np.int32)
+    h = np.zeros((rows, d))
+    h[:, :seen] = np.maximum(rng.normal(size=(rows, seen)) + lean * rng.random((rows, 1)) * W[:seen, y].T * np.sqrt(seen), 0.0)
+    W[seen:] += common * rng.normal(size=(d - seen, 1)) / np.sqrt(seen)
+    to = lambda x: torch.from_numpy(x.astype(np.float32)).to(DT[dtype])
+    return to(h), to(W), (0.1 * rng.normal(size=C)).astype(np.float32), y
+
+
+def dh_and_bound(h, W, b, y, inv_n, coarse):
+    """float64: dh and a bound for it as bf16.  With p the other classes' probabilities, q = p / sum p and t = sum p: dh = inv_n t (sum q W - W_y).
+      * the rounding of the result: v |dh|
+      * factors p (1 + e) weighted against their own sum: what classes' weights have in common cancels, sum e q |W_c - sum q W| is left.  e is v for q up to
+        ``coarse`` and 2 v^2 for the others; and 4 dz for all, dz being how far a logit is off, (d + 3) u of its terms
+      * t as a whole: 8 dz and the rounding of a sum of C terms, of dh
+      * fp32 sums of C terms, and the difference of t sum q W and t W_y: (C + 64) u of their magnitudes"""
+    h, W, b = h.double().numpy(), W.double().numpy(), b.astype(np.float64)
+    n, d = h.shape
+    C = W.shape[1]
+    z = h @ W + b
+    z -= z.max(1, keepdims=True)
+    p = np.exp(z)
+    own = p[np.arange(n), y].copy()
+    p[np.arange(n), y] = 0.0
+    o = p.sum(1)
+    t, q = inv_n * o / (o + own), p / o[:, None]
+    mean = q @ W.T
+    dh = t[:, None] * (mean - W[:, y].T)
+    dz = (d + 3) * U * (np.abs(h) @ np.abs(W) + np.abs(b)).max(1)[:, None]
+    e = np.where(q <= coarse, V / (1 - V), 2 * V * V) + 4 * dz
+    away = np.empty((n, d))
+    for k in range(d):
+        away[:, k] = (e * q * np.abs(W[k][None, :] - mean[:, k:k + 1])).sum(1)
+    mag = q @ np.abs(W).T + np.abs(W[:, y].T)
+    return dh, V * np.abs(dh) + ((8 * dz + (C + 64) * U) * np.abs(dh) + t[:, None] * (away + (C + 64) * U * mag)) * (1 + V)
+
+
+@pytest.mark.parametrize("rows,d,C,common", [(2000, 256, 41, 0), (2000, 256, 41, 16), (900, 128, 172, 4), (700, 100, 300, 16), (900, 64, 60, 64), (40, 200, 3000, 64),
+                                             (300, 256, 2100, 16), (517, 33, 5000, 16), (9001, 250, 41, 16), (1, 64, 2, 16)])
+def test_input_gradients_to_the_rounding_of_their_type(rows, d, C, common):
+    """bf16 rows of up to 256 columns: dh is as good as its type, also where all classes' weights have most in common and cancel."""
+    h, W, b, y = leaning(rows, d, C, "bf16", rows + d + C, common)
+    want, bound = dh_and_bound(h, W, b, y, 1.0 / 64, COARSE)
+    got = run_head(h, W, b, y, None, 1.0 / 64, "bf16")["dh"]
+    off = np.abs(got - want)
+    assert np.all(off <= bound), (float((off / bound).max()), float(np.linalg.norm(off) / np.linalg.norm(want)))
+
+
+def test_probabilities_that_all_round_the_same_way():
+    """All other classes have the same logit and the label's a larger one: every factor is the same number, and rounds by the same part of itself.  Weighted against
+    their own sum nothing of that is left, however coarse the factors."""
+    rows, d, C = 200, 64, 2000
+    rng = np.random.default_rng(3)
+    W = torch.from_numpy((8.0 + 0.5 * rng.integers(-2, 3, size=(d, C))).astype(np.float32)).bfloat16()
+    W[0] = 0.0
+    W[0, 0] = 1.3
+    h = torch.zeros(rows, d, dtype=torch.bfloat16)
+    h[:, 0] = torch.from_numpy((1.0 + rng.random(rows)).astype(np.float32))
+    b, y = np.zeros(C, np.float32), np.zeros(rows, np.int32)
+    want, bound = dh_and_bound(h, W, b, y, 1.0, 0.0)
+    got = run_head(h, W, b, y, None, 1.0, "bf16")["dh"]
+    off = np.abs(got - want)
+    assert np.all(off <= bound), float((off / bound).max())
