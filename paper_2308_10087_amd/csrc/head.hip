@@ -343,7 +343,7 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
   const StageWeightsArgs w{c.W, p.d, p.C, at(p.Wt), p.Kp, at(p.Wn), p.Cp};
   HEAD_TRY(launch_stage_weights(&w, 1, p.dtype, nullptr, s));
   const bool one = p.piece >= p.C, own32 = p.own32;
-  if (c.dh && !one && !own32 && !p.turned) HEAD_TRY(launch_fill_zero(at(p.zeros), sizeof(float) * (size_t)round_up(p.d, 64), s));
+  if (c.dh && (!one || p.dtype == GNNSTAGE_BF16) && !own32 && !p.turned) HEAD_TRY(launch_fill_zero(at(p.zeros), sizeof(float) * (size_t)round_up(p.d, 64), s));
   float *logits = reinterpret_cast<float *>(at(p.logits)), *acc = reinterpret_cast<float *>(at(p.acc));
   int32_t *label = reinterpret_cast<int32_t *>(at(p.label));
   RowState *state = reinterpret_cast<RowState *>(at(p.state));
@@ -413,18 +413,25 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
           hipLaunchKernelGGL(piece_grad_kernel<1>, dim3(waves), dim3(256), 0, s, logits, p.ld, c.bias, label, M, c0, n, c.inv_n, state, high, low, lowest);
         HEAD_TRY(hipGetLastError());
       }
+      // bf16: dh from the first two of the gradients' numbers, 2^-16 of each.  (From the first alone, 2^-8 of the label's too: 2,000 x 500 x 41 classes, relative error
+      // 2.2e-3 against 1.66e-3 with both, bf16's own, and 2.4e-2 where all classes share a column of 16 times what tells them apart; a sixth product costs
+      // 20,000 x 500 x 2,000 785 -> 944 us, 3,000 x 1,000 x 9,000 3,335 -> 3,670.)
+      const int parts = high ? 2 : 1;
       if (c.dh && p.turned) {
         if (c0 == 0) HEAD_TRY(launch_fill_zero(acc, sizeof(float) * (size_t)M * p.d, s));
         const dim3 grid((unsigned)((n + 31) / 32), (unsigned)((M + 31) / 32));
-        if (high)
-          hipLaunchKernelGGL(turn_kernel<bf16_t>, grid, dim3(256), 0, s, high, p.ld, (int)M, n, reinterpret_cast<bf16_t *>(at(p.turn)), p.ld_turned);
-        else
-          hipLaunchKernelGGL(turn_kernel<float>, grid, dim3(256), 0, s, logits, p.ld, (int)M, n, reinterpret_cast<float *>(at(p.turn)), p.ld_turned);
-        HEAD_TRY(hipGetLastError());
-        if (own32) {
-          HEAD_TRY(launch_tn32(reinterpret_cast<const float *>(at(p.turn)), p.ld_turned, reinterpret_cast<const float *>(at(p.Wt)) + (size_t)c0 * p.Kp, p.Kp, n,
-                               (int)M, p.d, acc, p.d, nullptr, reinterpret_cast<float *>(at(p.partial)), nullptr, p.max_splits_turned, s));
-        } else {
+        for (int part = 0; part < parts; ++part) {
+          if (high)
+            hipLaunchKernelGGL(turn_kernel<bf16_t>, grid, dim3(256), 0, s, part == 0 ? high : low, p.ld, (int)M, n, reinterpret_cast<bf16_t *>(at(p.turn)),
+                               p.ld_turned);
+          else
+            hipLaunchKernelGGL(turn_kernel<float>, grid, dim3(256), 0, s, logits, p.ld, (int)M, n, reinterpret_cast<float *>(at(p.turn)), p.ld_turned);
+          HEAD_TRY(hipGetLastError());
+          if (own32) {
+            HEAD_TRY(launch_tn32(reinterpret_cast<const float *>(at(p.turn)), p.ld_turned, reinterpret_cast<const float *>(at(p.Wt)) + (size_t)c0 * p.Kp, p.Kp,
+                                 n, (int)M, p.d, acc, p.d, nullptr, reinterpret_cast<float *>(at(p.partial)), nullptr, p.max_splits_turned, s));
+            continue;
+          }
           GemmTnArgs t{};
           t.A = at(p.turn);
           t.a_dtype = p.dtype;
@@ -451,25 +458,27 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
         continue;
       }
       if (c.dh && !p.turned) {
-        GemmNtArgs g{};
-        g.A = high ? (const void *)high : logits;  // dh is of the rows' type: the rounding of its factors to bf16 is below its own
-        g.a_dtype = p.dtype;
-        g.lda = p.ld;
-        g.Bt = at(p.Wn) + (size_t)c0 * p.elt;
-        g.ldb = p.Cp;
-        g.M = (int)M;
-        g.N = p.d;
-        g.K = n;
-        g.Kp = round_up(n, 8);
-        g.epilogue = c0 == 0 ? EPI_PLAIN : EPI_RES;
-        g.bias = reinterpret_cast<const float *>(at(p.zeros));
-        g.aux = acc;
-        g.aux_dtype = DT_F32;
-        g.aux_ld = p.d;
-        g.out = acc;
-        g.out_dtype = DT_F32;
-        g.out_ld = p.d;
-        HEAD_TRY(launch_gemm_nt(g, p.dtype, s));
+        for (int part = 0; part < parts; ++part) {
+          GemmNtArgs g{};
+          g.A = !high ? (const void *)logits : part == 0 ? high : low;
+          g.a_dtype = p.dtype;
+          g.lda = p.ld;
+          g.Bt = at(p.Wn) + (size_t)c0 * p.elt;
+          g.ldb = p.Cp;
+          g.M = (int)M;
+          g.N = p.d;
+          g.K = n;
+          g.Kp = round_up(n, 8);
+          g.epilogue = c0 == 0 && part == 0 ? EPI_PLAIN : EPI_RES;
+          g.bias = reinterpret_cast<const float *>(at(p.zeros));
+          g.aux = acc;
+          g.aux_dtype = DT_F32;
+          g.aux_ld = p.d;
+          g.out = acc;
+          g.out_dtype = DT_F32;
+          g.out_ld = p.d;
+          HEAD_TRY(launch_gemm_nt(g, p.dtype, s));
+        }
       }
       if (c.dW || c.db) {
         const bool whole = one && c.dW;

@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_head_rows8 import DT, U, V, counts, head_formula, run_head
+from test_gpu_head_rows8 import DT, U, V, head_formula, run_head
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +82,22 @@ def test_probabilities_that_all_round_the_same_way():
     got = run_head(h, W, b, y, None, 1.0, "bf16")["dh"]
     off = np.abs(got - want)
     assert np.all(off <= bound), float((off / bound).max())
+
+
+@pytest.mark.parametrize("rows,d,C,common", [(2000, 500, 41, 0), (2000, 500, 41, 16), (700, 300, 1000, 4), (300, 500, 9001, 0), (37, 264, 9001, 64), (4200, 264, 9001, 4),
+                                             (1, 1000, 2, 16)])
+def test_input_gradients_of_wide_rows(rows, d, C, common):
+    """bf16 rows of more than 256 columns: every g, the label's too, enters dh as the sum of two bf16 numbers, v^2 of it off at most; where classes are many, rows few or
+    many, or both in pieces.  Beside that dh_and_bound's errors, of terms as they are: nothing cancels on its own here."""
+    h, W, b, y = leaning(rows, d, C, "bf16", rows + d + C, common)
+    # logits are made of multiples of 2^-9 below 2^14: every sum of theirs is exact, and what comes after is off by a few roundings of theirs
+    h, W[:(d + 1) // 2], b = (h * 8).round() / 8, (W[:(d + 1) // 2] * 64).round() / 64, np.round(b * 64) / 64
+    z = h.double().numpy() @ W.double().numpy() + b
+    assert np.abs(h.double().numpy()).max() < 32 and float(W[:(d + 1) // 2].abs().max()) < 4 and np.abs(z).max() < 2 ** 12
+    inv_n = 1.0 / 64
+    want, mag = head_formula(h.double().numpy(), W.double().numpy(), b.astype(np.float64), y, np.ones(rows, bool), inv_n)
+    dz = 4 * U * (1 + z.max(1) - z.min(1))[:, None]
+    got = run_head(h, W, b, y, None, inv_n, "bf16")["dh"]
+    bound = V * np.abs(want["dh"]) + (V * V + 12 * dz + (2 * C + 64) * U) * mag["dh"] * (1 + V)
+    off = np.abs(got - want["dh"])
+    assert np.all(off <= bound), (float((off / bound).max()), float(np.linalg.norm(off) / np.linalg.norm(want["dh"])))
