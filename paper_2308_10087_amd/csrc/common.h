@@ -364,6 +364,7 @@ struct GemmNtArgs {
   float mask_scale = 1.f;  // EPI_MASK: what passes the mask is scaled (1 / (1 - rate) of that dropout)
   LnDropout drop{};        // EPI_FWD_GCN / EPI_FWD_ADD: dropout of the layer's output (threshold 0: none)
   int32_t ws_min_rows = 65536;  // rows from which the weight-stationary kernel is used (tests force it on small inputs)
+  int32_t blocks = 0;           // fp32, EPI_PLAIN / EPI_RES: sums in chains of 64 or 192 products, which are added up, instead of one chain in the order of k
 };
 int launch_gemm_nt(const GemmNtArgs &a, int compute_dtype, hipStream_t s);
 

@@ -1146,7 +1146,9 @@ __device__ inline void epilogue_store4_f32(const GemmNtArgs &a, int m, int n, co
 // 72 us on the vector ALU, 11.5 us here.  1,078 x 100 x 100: 13 -> 4.6 us.
 // Q = 2: for products of many tiles; half the operand bytes per product through L2.  Taken from 512 of its 64 x 64 workgroup
 // tiles on.
-template <int Q, int EPI>
+// BLOCKS: sums on which no ReLU decides, in chains of 16 D products that are added up, which is nearer to 64 bits where they are long and takes no longer: the loss
+// head's row gradients over 8,192 classes are off by 1.64e-6 in one chain and 2.9e-7 so; 20,000 x 256 x 8,000 3,472 / 3,315 us, 5,000 x 64 x 8,000 351 / 351.
+template <int Q, int EPI, bool BLOCKS = false>
 __global__ __launch_bounds__(256) void gemm_nt_f32_kernel(const GemmNtArgs a) {
   constexpr int T = 32 * Q;          // rows and columns of a workgroup's tile
   constexpr int D = Q == 1 ? 12 : 4; // groups of 16 reduction elements in flight per wave
@@ -1181,6 +1183,13 @@ __global__ __launch_bounds__(256) void gemm_nt_f32_kernel(const GemmNtArgs a) {
   for (int x = 0; x < Q; ++x)
 #pragma unroll
     for (int y = 0; y < Q; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 sum[Q][Q];  // BLOCKS: of the chains that are closed
+  if constexpr (BLOCKS) {
+#pragma unroll
+    for (int x = 0; x < Q; ++x)
+#pragma unroll
+      for (int y = 0; y < Q; ++y) sum[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   f32x4 fa[D][Q], fb[D][Q];  // loads in flight
   f32x4 pa[Q], pb[Q];        // the last, partial group
   f32x4 x4[Q], y4[Q];        // operands of the next products: element s for step s
@@ -1262,6 +1271,15 @@ __global__ __launch_bounds__(256) void gemm_nt_f32_kernel(const GemmNtArgs a) {
         load(i + D + u < cnt ? i + D + u : cnt - 1, u);  // slot u is held already
         step(fa[(u + 1) % D], fb[(u + 1) % D]);
       }
+      if constexpr (BLOCKS) {
+#pragma unroll
+        for (int x = 0; x < Q; ++x)
+#pragma unroll
+          for (int y = 0; y < Q; ++y) {
+            sum[x][y] += acc[x][y];
+            acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+      }
     }
 #pragma unroll
     for (int u = 0; u < D; ++u)
@@ -1271,6 +1289,12 @@ __global__ __launch_bounds__(256) void gemm_nt_f32_kernel(const GemmNtArgs a) {
     turn(pa, pb);
   }
   mul(x4, y4);
+  if constexpr (BLOCKS) {
+#pragma unroll
+    for (int x = 0; x < Q; ++x)
+#pragma unroll
+      for (int y = 0; y < Q; ++y) acc[x][y] += sum[x][y];
+  }
   // element e of lane l of an instruction tile is row 4 * (l / 16) + e, column l % 16
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -1605,6 +1629,14 @@ int launch_gemm_nt(const GemmNtArgs &a_in, int compute_dtype, hipStream_t s) {
 #undef NT_F32
     if (a.epilogue < 0 || a.epilogue > 6) return hipErrorInvalidValue;
     fn = table[wide][a.epilogue];
+    if (a.blocks) {
+      if (a.epilogue == EPI_PLAIN)
+        fn = wide ? gemm_nt_f32_kernel<2, EPI_PLAIN, true> : gemm_nt_f32_kernel<1, EPI_PLAIN, true>;
+      else if (a.epilogue == EPI_RES)
+        fn = wide ? gemm_nt_f32_kernel<2, EPI_RES, true> : gemm_nt_f32_kernel<1, EPI_RES, true>;
+      else
+        return hipErrorInvalidValue;
+    }
     gx = (unsigned)(((long long)((a.M + T - 1) / T) * ((a.N + T - 1) / T) + 7) / 8 * 8);
   } else {
     const bool has_aux = a.epilogue == EPI_FWD_GCNII || a.epilogue == EPI_MASK || a.epilogue == EPI_DGRAD_GCNII ||

@@ -378,6 +378,7 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
       g.K = p.d;
       g.Kp = p.Kp;
       g.epilogue = EPI_PLAIN;
+      g.blocks = p.dtype == GNNSTAGE_F32;
       g.out = logits;
       g.out_dtype = DT_F32;
       g.out_ld = p.ld;
@@ -470,6 +471,7 @@ int run_in_pieces(const Plan &p, const Call &c, hipStream_t s) {
           g.K = n;
           g.Kp = round_up(n, 8);
           g.epilogue = c0 == 0 && part == 0 ? EPI_PLAIN : EPI_RES;
+          g.blocks = p.dtype == GNNSTAGE_F32;
           g.bias = reinterpret_cast<const float *>(at(p.zeros));
           g.aux = acc;
           g.aux_dtype = DT_F32;

@@ -101,3 +101,22 @@ def test_input_gradients_of_wide_rows(rows, d, C, common):
     bound = V * np.abs(want["dh"]) + (V * V + 12 * dz + (2 * C + 64) * U) * mag["dh"] * (1 + V)
     off = np.abs(got - want["dh"])
     assert np.all(off <= bound), (float((off / bound).max()), float(np.linalg.norm(off) / np.linalg.norm(want["dh"])))
+
+
+@pytest.mark.parametrize("rows,d,C", [(500, 64, 8000), (70, 300, 8000), (9001, 256, 6000), (8400, 33, 8300), (300, 64, 20001), (700, 390, 12000), (5, 1000, 4000)])
+def test_long_sums_of_fp32_input_gradients(rows, d, C):
+    """All logits are equal, so dh is a sum of C - 1 equal terms and the label's: in one chain the additions' roundings go the same way for thousands of terms.  In
+    chains of at most 256 that are added up, or in tiles of them, a sum is off by (256 + C / 64 + 64) u; g by a few roundings, its own sum being one of ones."""
+    rng = np.random.default_rng(rows)
+    w, v = (1.0 + rng.random(d)).astype(np.float32), (-1.0 - rng.random(d)).astype(np.float32)
+    W = torch.from_numpy(np.repeat(w[:, None], C, 1))
+    W[:, 0] = torch.from_numpy(v)
+    y = np.zeros(rows, np.int32)
+    got = run_head(torch.zeros(rows, d), W, None, y, None, 1.0 / 64, "f32")
+    own = (C - 1) / C / 64
+    want = own * (w.astype(np.float64) - v)
+    mag = own * (w.astype(np.float64) + np.abs(v))
+    off = np.abs(got["dh"] - want).max(0)
+    bound = (256 + C / 64 + 64) * U * mag
+    assert np.all(off <= bound), float((off / bound).max())
+    assert np.abs(got["loss"] - np.log(C)).max() <= 8 * U * np.log(C)
