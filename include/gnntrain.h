@@ -122,8 +122,9 @@ int gnntrain_softmax_xent(const float *logits, int32_t ld, const float *bias, co
  * dh (of dtype, leading dimension ld_dh), dW (fp32 d x n_classes), db (fp32 n_classes): DEVICE, each may be NULL; all NULL: the losses
  * alone.  Outputs may not overlap inputs (dh == h is refused).  d in [1, 65534], n_classes in [1, 2^24], d * n_classes at most 2^33.
  * bf16 products have fp32 sums.  Their factors: in dh every g is the sum of two bf16 numbers (2^-16 of itself), but of up to 256 columns a probability
- * of less than 1/32 of its row's others may be one (2^-8 of itself, where what the weights have in common cancels all the same); the g in dW's are held to
- * 16 bits at least, those of more than 16,384 labelled rows, all of their bits otherwise.  Sums are added in a fixed order: the same call gives the same bits.
+ * of less than 1/32 of its row's others may be one (2^-8 of itself, where what the weights have in common cancels all the same); the g in dW's
+ * are the sum of two (2^-16), and where a slab of 2^20 rows has at most 16,384 labelled ones, or fewer than 128 a class, of three (all bits) in blocks of 32 rows and
+ * 32 classes in which some |g| is above inv_n_train / 64; wider rows' g in dW's have all bits.  Sums are added in a fixed order: the same call gives the same bits.
  * workspace: DEVICE, 256-byte aligned, of gnntrain_head_xent_workspace_size(); written by the call, nothing in it has to be
  * cleared or kept.  Calls that overlap in time need workspaces of their own, and so do graphs that are replayed side by side.
  * The call only launches kernels (asynchronous, may be captured).  Message of an error: gnntrain_last_error(NULL). */

@@ -544,8 +544,9 @@ typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896f;
-constexpr float kExactFrom = 1.f / 64;  // (1 / 2 takes as long)
+constexpr float kExactFrom = 1.f / 64;  // of g times the number of rows that inv_n stands for (1 / 2 takes as long)
 constexpr int kExactRows = 16384;
+constexpr int kExactPerClass = 128;
 constexpr float kCoarseTo = 1.f / 32;  // see mean_scale
 constexpr float kNoMax = -3.4028234663852886e38f;  // the least number: of a row that has seen no more than minus infinity
 // exp(z - m): the difference first, so that it is exact for the logits that count, however large they are
@@ -1009,10 +1010,17 @@ struct ClassesArgs {
 __device__ inline int64_t run_begin(int64_t total, int groups, int g) { return total * g / groups; }
 
 //
-// EXACT: g with all of their bits.  16 bits are 2e-6 of a single term of dW; of a sum over many rows that is less than the rounding of the sum in fp32, over few rows
-// it is not.  So where the labelled rows are kExactRows at most, the tiles with large g (a label's, a sure row's: what a column of dW consists of, and in few
-// tiles where the classes are many) go around once more for the third bf16 number.  Relative error of dW, 16 bits / all: 370 rows of 96 classes 1.6e-6 / 2.3e-7,
-// 517 of 50,021 4.5e-7 / 2.4e-7 (183 / 190 us); 18,000 of 100,003 1.0e-6 / 9.8e-7 (4.0 / 4.2 ms), where fp32 products have 1.7e-6.
+// EXACT: 16 bits of g are up to 2^-16 of a single term of dW.  Added up over many labelled rows of a class that is less than what an fp32 product's own sum is off by;
+// over few it is not.  So where a slab's labelled rows are kExactRows at most, or fewer than kExactPerClass a class, the tiles with large g (a label's, a sure
+// row's: what a column of dW consists of where rows have its class) go around once more for the third bf16 number, which is all of a g's bits; g in tiles
+// without a large one keep 16.  Relative error of dW (norm / worst column), 16 bits, all, the fp32 products of the plain form:
+//   370 rows of 96 classes              1.6e-6          2.3e-7          2.3e-7
+//   17,000 of 1,000   (17 a class)      1.2e-6 / 4.3e-6 3.0e-7 / 0.6e-6 7.6e-7 / 1.9e-6     calls at width 256: 138 / 152 us
+//   40,000 of 1,000   (40)              1.0e-6 / 3.7e-6 4.4e-7 / 1.0e-6 1.0e-6 / 2.2e-6                         180 / 236
+//   17,000 of 172     (99)              7.0e-7 / 2.2e-6 3.3e-7 / 0.7e-6 1.4e-6 / 2.0e-6     width 128:           59 / 65
+//   400,000 of 1,000  (400)             5.5e-7 / 2.2e-6 4.6e-7 / 1.4e-6 1.4e-6 / 3.0e-6                         1,023 / 1,477
+//   120,000 of 41     (2,900)           2.8e-7 / 1.0e-6 2.2e-7 / 0.6e-6 1.4e-6 / 1.7e-6                         108 / 128
+// (18,010 of 100,003, width 256: 4,000 / 4,110 us; 23,300 of 10,007, width 100: 385 / 422.)
 template <int DP, bool DIRECT, bool EXACT, int IN_REGS>
 __global__ __launch_bounds__(256, kPerUnit<DP>) void head_classes_kernel(const ClassesArgs a) {
   typedef Geometry<DP> G;
@@ -1030,7 +1038,7 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_classes_kernel(const C
   __shared__ __attribute__((aligned(16))) char shared[Own::in_lds > 0 ? 4 * Own::in_lds * 1024 : 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
   const int row_steps = a.meta->row_steps, groups = a.meta->groups, n = a.meta->n, group = blockIdx.x;
-  if (group >= groups || EXACT != (n <= kExactRows)) return;
+  if (group >= groups || EXACT != (n <= kExactRows || n < (int64_t)kExactPerClass * a.C)) return;
   const int64_t total = (int64_t)a.class_tiles * row_steps, run0 = run_begin(total, groups, group), run1 = run_begin(total, groups, group + 1);
   Places<DP> at(wave, lane);
   int32_t index[DIRECT ? G::loads : 1];  // of the rows that this lane loads next
@@ -1537,7 +1545,7 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   const int64_t groups = std::max<int64_t>(round_of(p.DP), p.class_tiles);  // at most
   hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, true, kClassesInRegs<DP>>), dim3((unsigned)groups), dim3(256), 0, s, k);
   HEAD_TRY(hipGetLastError());
-  if (rows > kExactRows) {  // how many have labels is known to the device: one of the two returns at once
+  if (rows > kExactRows && rows >= (int64_t)kExactPerClass * p.C) {  // how many have labels is known to the device: one of the two returns at once
     hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, false, kClassesInRegs<DP>>), dim3((unsigned)groups), dim3(256), 0, s, k);
     HEAD_TRY(hipGetLastError());
   }

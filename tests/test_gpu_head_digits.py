@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_head_rows8 import DT, U, V, head_formula, run_head
+from test_gpu_head_rows8 import DT, U, V, check_head, counts, head_formula, head_inputs, run_head
 
 pytestmark = pytest.mark.gpu
 
@@ -120,3 +120,56 @@ def test_long_sums_of_fp32_input_gradients(rows, d, C):
     bound = (256 + C / 64 + 64) * U * mag
     assert np.all(off <= bound), float((off / bound).max())
     assert np.abs(got["loss"] - np.log(C)).max() <= 8 * U * np.log(C)
+
+
+def one_hot(rows, d, C, seed, active=8):
+    """Rows of one number each in a column of its own, then rows of zeros: an element of dW is one term and zeros.  All classes but ``active`` are left out.  Logits are
+    multiples of 2^-13 within -3 and 3: exact."""
+    rng = np.random.default_rng(seed)
+    at = np.sort(rng.choice(C, active, replace=False))
+    h = np.zeros((rows, d), np.float32)
+    k = min(rows, d)
+    h[np.arange(k), np.arange(k)] = 1.0 + rng.integers(0, 128, size=k) / 128
+    W = rng.integers(-64, 65, size=(d, C)) / 64
+    b = np.full(C, -np.inf, np.float32)
+    b[at] = rng.integers(-16, 17, size=active) / 16
+    y = at[rng.integers(0, active, size=rows)].astype(np.int32)
+    return torch.from_numpy(h).bfloat16(), torch.from_numpy(W.astype(np.float32)).bfloat16(), b, y, at
+
+
+@pytest.mark.parametrize("rows,d,C", [(1, 64, 8), (300, 256, 8), (300, 100, 40), (129, 128, 70), (16384, 200, 64), (17000, 256, 200), (20000, 128, 300), (20000, 40, 1000),
+                                      (60000, 100, 1000), (300, 300, 40), (17000, 300, 200)])
+def test_weight_gradients_have_all_bits_where_a_class_has_few_rows(rows, d, C):
+    """Every element of dW is h_ik g_ic inv_n with h and inv_n short numbers, so it is as good as g, and g's of a row's own class are large: all bits.  g is off by its
+    exponent, 12 at most, whose last digit is 16 u: 2 * 16 u ln 2 for it and its part log2 of the sum; by its sum of 8 terms, 8 u; by two functions, 8 u: 40 u."""
+    h, W, b, y, at = one_hot(rows, d, C, rows + d + C)
+    want, _ = head_formula(h.double().numpy(), W.double().numpy(), b.astype(np.float64), y, np.ones(rows, bool), 1.0 / 64)
+    got = run_head(h, W, b, y, None, 1.0 / 64, "bf16", grads=("dW", "db"))["dW"]
+    k = np.arange(min(rows, d))
+    own = (k, y[k])
+    off = np.abs(got / np.where(want["dW"] == 0, 1.0, want["dW"]) - (want["dW"] != 0))
+    assert off[own].max() <= 40 * U, float(off[own].max() / U)
+    assert off[k].max() <= 40 * U + V * V
+    assert np.all(got[want["dW"] == 0] == 0)
+
+
+@pytest.mark.parametrize("rows,d,C", [(33, 128, 8200), (257, 64, 20011), (1, 256, 50021), (700, 250, 9001), (90, 300, 9001), (17500, 100, 8300)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norms_over_many_classes(rows, d, C, dtype):
+    """A sum of C roundings of random signs is 4 sqrt(C) u off at most (four of its standard deviations); g to 16 bits 2^-16; logits of d terms 4 sqrt(d) u of
+    their magnitudes, which is what g is off by.  As norms: what only the worst case of every rounding allows does not pass here."""
+    h, W, b, y, mask = head_inputs(rows, d, C, dtype, rows + C, "some" if rows > 1 else "all")
+    on = counts(y, mask, C)
+    inv_n = 1.0 / max(1, int(on.sum()))
+    want, mag = head_formula(h.double().numpy(), W.double().numpy(), b.astype(np.float64), y, on, inv_n)
+    got = run_head(h, W, b, y, mask, inv_n, dtype)
+    sums = 4 * np.sqrt(C) * U + 4 * np.sqrt(d) * U * float(mag["z"].max()) + 64 * U
+    for key, more in (("loss", 0.0), ("dW", V * V), ("db", V * V), ("dh", V if dtype == "bf16" else 0.0)):
+        rel = np.linalg.norm(got[key] - want[key]) / np.linalg.norm(want[key])
+        assert rel <= sums + 4 * np.sqrt(max(rows, C)) * U + more, (key, rel)
+
+
+@pytest.mark.parametrize("d", [256, 200, 128, 64])
+def test_weight_gradients_of_classes_with_many_rows(d):
+    """More than 16,384 labelled rows and more than 128 a class: two bf16 numbers of every g, of rows as they are and packed."""
+    check_head(34000, d, 100, "bf16", "some")
