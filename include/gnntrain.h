@@ -76,7 +76,8 @@ typedef struct {
 
 /* Device bytes the loop needs: optimiser moments, logits of up to 131,072 vertices, gradient of the logits and
  * gradient rows of the last level for all vertices, per-vertex losses, staged head weights, split-reduction
- * scratch (head_fused: gnntrain_head_xent's workspace in the place of logits, their gradients, weights and scratch).  Host-only; 0 on an invalid descriptor. */
+ * scratch (head_fused: gnntrain_head_xent's workspace in the place of logits, their gradients, weights and scratch).  Host-only; 0 on an invalid descriptor
+ * (why: gnntrain_last_error(NULL)), also where the head refuses the last level's width or its product with n_classes. */
 size_t gnntrain_workspace_size(const gnntrain_desc *desc);
 
 /* Validates the descriptor against the stage handles (chaining of the level buffers, label range),

@@ -813,7 +813,7 @@ class GnnTrainer:
         d.head_fused = int(bool(head_fused))
         size = int(lib.gnntrain_workspace_size(C.byref(d)))
         if size == 0:
-            raise GnnStageError(-1, "gnntrain_workspace_size: invalid descriptor")
+            raise GnnStageError(-1, "gnntrain_workspace_size: " + lib.gnntrain_last_error(None).decode())
         self.workspace_bytes = size
         self.workspace = torch.empty(size, dtype=torch.uint8, device=device)
         d.workspace, d.workspace_bytes = self.workspace.data_ptr(), size

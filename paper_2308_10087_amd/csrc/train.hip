@@ -194,13 +194,14 @@ UpdateArgs adam_args(float lr, float b1, float b2, float eps, float wd, int64_t 
 
 struct Layout {
   size_t m = 0, v = 0, logits = 0, dlogits = 0, dtop = 0, row_loss = 0, scratch = 0, loss = 0, Wt = 0, Wn = 0, gemm_partial = 0,
-         bias_partial = 0, head = 0, head_bytes = 0, total = 0;
+         bias_partial = 0, head = 0, total = 0;
 };
 
 struct Dims {
   int64_t n = 0, head_rows = 0, n_param_elems = 0;  // head_rows: of one block of the head's work
   int K = 0, d_top = 0, C = 0, Cp = 0, Kp = 0, dtype = 0, elt = 4;
   bool fused = false;
+  size_t head_bytes = 0;  // fused: the head's workspace
 };
 
 bool read_dims(const gnntrain_desc *d, Dims &x, std::string &err) {
@@ -227,6 +228,10 @@ bool read_dims(const gnntrain_desc *d, Dims &x, std::string &err) {
   x.Cp = round_up(x.C, 8);
   x.Kp = round_up(x.d_top, 8);
   x.head_rows = std::min<int64_t>(x.n, 131072);
+  if (x.fused) {
+    x.head_bytes = gnntrain_head_xent_workspace_size(x.n, x.d_top, x.C, x.dtype, 1);
+    if (x.head_bytes == 0) { err = gnntrain_last_error(nullptr); return false; }  // its own limits: of the last level's width, of the weights
+  }
   x.n_param_elems = 0;
   for (int i = 0; i < d->n_params; ++i) {
     const gnntrain_param &p = d->params[i];
@@ -257,8 +262,7 @@ Layout make_layout(const gnntrain_desc *d, const Dims &x) {
   l.scratch = take(sizeof(float) * 1024);
   l.loss = take(256);
   if (x.fused) {
-    l.head_bytes = gnntrain_head_xent_workspace_size(x.n, x.d_top, x.C, x.dtype, 1);
-    l.head = take(l.head_bytes);
+    l.head = take(x.head_bytes);
   } else {
     l.Wt = take((size_t)x.elt * x.C * x.Kp);
     l.Wn = take((size_t)x.elt * x.d_top * x.Cp);
@@ -444,7 +448,10 @@ extern "C" int gnntrain_sgd_step(float *p, const float *g, void *compute, int32_
 extern "C" size_t gnntrain_workspace_size(const gnntrain_desc *desc) try {
   Dims x;
   std::string err;
-  if (!read_dims(desc, x, err)) return 0;
+  if (!read_dims(desc, x, err)) {
+    train_error(GNNSTAGE_EINVAL, err);
+    return 0;
+  }
   return make_layout(desc, x).total;
 }
 GNNSTAGE_GUARD_SIZE
@@ -599,7 +606,7 @@ extern "C" int gnntrain_epoch(gnntrain_t *tr, int64_t epoch, float *loss, void *
   }
   if (x.fused) {
     const int rc = gnntrain_head_xent(tr->top, x.d_top, tr->head_W, cd, tr->head_b, tr->labels, tr->mask, x.n, x.d_top, x.C, inv_n, row_loss,
-                                      tr->at<char>(lay.dtop), x.d_top, tr->head_dW, tr->head_db, tr->at<char>(lay.head), lay.head_bytes, stream);
+                                      tr->at<char>(lay.dtop), x.d_top, tr->head_dW, tr->head_db, tr->at<char>(lay.head), x.head_bytes, stream);
     if (rc != GNNSTAGE_OK) return fail(tr, rc, gnntrain_last_error(nullptr));
   }
   const int64_t head_n = x.fused ? 0 : x.n;  // rows of the head in blocks
