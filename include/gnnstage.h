@@ -381,7 +381,7 @@ int gnnstage_profile_reset(gnnstage_t *st);
  *   gnnstage_rows8_store        q, scale from x (rows x d)
  *   gnnstage_rows8_load         x from q, scale
  *   gnnstage_rows8_weight_grad  dW (fp32 d x d_out) += X^T dY, dbias (fp32 d_out, may be NULL) += column sums of dY, with X the stored rows:
- *                               products of exactly the stored values, fp32 sums in a fixed order.  workspace: DEVICE, 256-byte aligned, of
+ *                               products of exactly the stored values, fp32 sums in a fixed order.  d * d_out at most 2^30 - 2^17.  workspace: DEVICE, 256-byte aligned, of
  *                               gnnstage_rows8_weight_grad_workspace_size() bytes, nothing to be cleared or kept; calls that overlap in time need
  *                               workspaces of their own.
  * They only launch kernels on hip_stream.  Message of an error: gnnstage_last_error(NULL).

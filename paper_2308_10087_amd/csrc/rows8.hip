@@ -153,6 +153,11 @@ bool sizes_ok(int64_t rows, int d, std::string &err) {
   if (d < 1 || d > 65536) { err = "a width must be in [1, 65536]"; return false; }
   return true;
 }
+// Of a weight gradient: what adds up the row splits has four threads per element of dW and dbias in one launch, below 2^32.
+bool outputs_ok(int d, int d_out, std::string &err) {
+  if ((int64_t)d * d_out > ((int64_t)1 << 30) - ((int64_t)1 << 17)) { err = "d * d_out must be at most 2^30 - 2^17"; return false; }
+  return true;
+}
 bool stored_ok(const void *q, int64_t ld_q, const void *scale, int64_t ld_s, int d, std::string &err) {
   if (!q || !scale) { err = "q and scale must not be NULL"; return false; }
   if ((reinterpret_cast<uintptr_t>(q) & 15u) || ld_q % 16 != 0) { err = "q must be 16-byte aligned, its leading dimension a multiple of 16"; return false; }
@@ -216,7 +221,7 @@ GNNSTAGE_GUARD_INT
 
 extern "C" size_t gnnstage_rows8_weight_grad_workspace_size(int64_t rows, int32_t d, int32_t d_out, int32_t dtype) try {
   std::string err;
-  if (!sizes_ok(rows, d, err) || !sizes_ok(rows, d_out, err)) {
+  if (!sizes_ok(rows, d, err) || !sizes_ok(rows, d_out, err) || !outputs_ok(d, d_out, err)) {
     stage_error(GNNSTAGE_EINVAL, "gnnstage_rows8_weight_grad: " + err);
     return 0;
   }
@@ -234,7 +239,7 @@ extern "C" int gnnstage_rows8_weight_grad(const int8_t *q, int64_t ld_q, const u
   const char *const me = "gnnstage_rows8_weight_grad: ";
   std::string err;
   if (dtype != GNNSTAGE_F32 && dtype != GNNSTAGE_BF16) return stage_error(GNNSTAGE_EINVAL, std::string(me) + "unknown dtype");
-  if (!sizes_ok(rows, d, err) || !sizes_ok(rows, d_out, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
+  if (!sizes_ok(rows, d, err) || !sizes_ok(rows, d_out, err) || !outputs_ok(d, d_out, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
   if (ld_dy < d_out || ld_dy > INT32_MAX || ld_q >= 1 << 24 || ld_s >= 1 << 24)
     return stage_error(GNNSTAGE_EINVAL, std::string(me) + "ld_dy is below d_out or beyond 2^31 - 1, or ld_q or ld_s beyond 2^24 - 1");
   if (rows == 0) return GNNSTAGE_OK;

@@ -48,6 +48,36 @@ def _trainer(rt, d_top, n_classes, bf16, fused):
     return [size, why, rc, lib.gnntrain_last_error(None).decode(), h.value is not None]
 
 
+def _buffer():
+    """A 256-byte aligned address that is never read: launches are listed, not run."""
+    some = np.zeros(4096, np.uint8)
+    return some, (some.ctypes.data + 255) // 256 * 256
+
+
+def _each(rt, what, cases):
+    return [globals()[what](rt, *c) for c in cases]
+
+
+def _weight_grad(rt, rows, d, d_out, bf16):
+    """Size, return code, message, launches."""
+    from paper_2308_10087_amd.binding import lib
+    keep, at = _buffer()
+    size = lib.gnnstage_rows8_weight_grad_workspace_size(rows, d, d_out, bf16)
+    rt.host_clear(-1)
+    rc = lib.gnnstage_rows8_weight_grad(at, (d + 31) // 32 * 32, at, (d + 31) // 32, at, bf16, d_out, rows, d, d_out, at, at, at, size or 1 << 60, None)
+    return [size, rc, lib.gnnstage_last_error(None).decode() if rc else "", rt.host_launches()]
+
+
+def _head(rt, rows, d, n_classes, bf16, grads):
+    from paper_2308_10087_amd.binding import lib
+    keep, at = _buffer()
+    size = lib.gnntrain_head_xent_workspace_size(rows, d, n_classes, bf16, grads)
+    rt.host_clear(-1)
+    g = at + 256 if grads else None
+    rc = lib.gnntrain_head_xent(at, d, at, bf16, at, at, None, rows, d, n_classes, 1.0, at, g, d, g, g, at, size, None)
+    return [size, rc, lib.gnntrain_last_error(None).decode() if rc else "", rt.host_launches()]
+
+
 if __name__ == "__main__":
     _rt = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
     from test_host_launches import _Launch
@@ -78,3 +108,24 @@ def test_the_loop_takes_what_its_head_takes(runtime):
         assert size > 0 and rc == 0 and made, again
     size, why, rc, _, made = _child(runtime, "_trainer", 64, 65537, False, 0)
     assert size == 0 and rc == -1 and not made and "65536" in why
+
+
+def test_the_largest_weight_gradients_can_be_launched(runtime):
+    cases = [(rows, d, d_out, bf16) for rows, d, d_out in [(100, 65536, 16382), (100, 16382, 65536), (5, 32767, 32764), (1 << 31, 65536, 1), (3, 1, 65536)] for bf16 in (0, 1)]
+    for c, (size, rc, why, launches) in zip(cases, _child(runtime, "_each", "_weight_grad", cases)):
+        assert size > 0 and rc == 0 and launches > 0, (c, why)
+
+
+def test_larger_weight_gradients_are_refused_before_anything_runs(runtime):
+    cases = [(rows, d, d_out, bf16) for rows, d, d_out in [(100, 65536, 16385), (100, 65536, 16383), (100, 16385, 65536), (1, 65536, 65536)] for bf16 in (0, 1)]
+    for c, (size, rc, why, launches) in zip(cases, _child(runtime, "_each", "_weight_grad", cases)):
+        assert size == 0 and rc == -1 and "2^30" in why and launches == 0, (c, size, rc, why)
+
+
+def test_heads_at_their_limits_can_be_launched(runtime):
+    """Every launch is one that the runtime takes: the widest rows, the most classes, the most weights, several slabs, few rows."""
+    cases = [c + (bf16, grads) for c in [(1, 1, 1), (1, 65534, 131072), (1, 512, 1 << 24), (300, 512, 1 << 24), (5000, 8, 1 << 24), (2200001, 256, 47), (2200001, 300, 47),
+                                         (140000, 65534, 2), (140000, 1, 200000), (4096, 65534, 8192), (4097, 40000, 8192), (1 << 21, 1, 1)]
+             for bf16 in (0, 1) for grads in (0, 1)]
+    for c, (size, rc, why, launches) in zip(cases, _child(runtime, "_each", "_head", cases)):
+        assert size > 0 and rc == 0 and launches > 0, (c, why)
