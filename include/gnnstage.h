@@ -230,7 +230,8 @@ int gnnstage_set_dropout_rate(gnnstage_t *st, float dropout_p);
 /* Synchronises the device and frees the handle (the workspace stays with the caller). */
 int gnnstage_destroy(gnnstage_t *st);
 
-/* Message for the last error on this handle (or, with NULL, of the last failed create). */
+/* Message for the last error on this handle (or, with NULL, of the calling thread's last failed create or call without a handle; it stays readable until that
+ * thread's next one). */
 const char *gnnstage_last_error(const gnnstage_t *st);
 
 /*

@@ -94,6 +94,7 @@ int gnntrain_epoch(gnntrain_t *tr, int64_t epoch, float *loss, void *hip_stream)
 int gnntrain_last_order(const gnntrain_t *tr, int32_t *order);
 
 int gnntrain_destroy(gnntrain_t *tr);
+/* Of this handle, or, with NULL, of the calling thread's last failed call without one (readable until that thread's next one). */
 const char *gnntrain_last_error(const gnntrain_t *tr);
 
 /* ---- the steps of the loop, exported one by one ------------------------------------------------- */

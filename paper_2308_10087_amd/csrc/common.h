@@ -492,7 +492,7 @@ constexpr int kFills = 32;
 int launch_gcn_norm(const int64_t *ptr, const uint32_t *pidx, int vbits, const int64_t *len_ptr, int64_t n,
                     float *val, hipStream_t s);
 
-// The last error of entry points without a handle: what gnntrain_last_error(NULL) and gnnstage_last_error(NULL) tell.  Return code.
+// The calling thread's last error of entry points without a handle: what gnntrain_last_error(NULL) and gnnstage_last_error(NULL) tell.  Return code.
 int train_error(int code, const std::string &msg);
 int stage_error(int code, const std::string &msg);
 

@@ -31,7 +31,7 @@ constexpr int64_t kSelfRows = 65536;
 // 12 k 128 / 130, 24 k 173 / 164.  Chunk calls of 75 rows of width 256: 2,160 / 2,613 us for 40 of them.
 constexpr int64_t kShortRowsPerColumn = 64;
 
-std::string g_create_error;
+thread_local std::string g_create_error;  // of calls without a handle: threads may be refused at once
 
 // Measurement and test switches.  Defaults are the product path.  The environment is read ONCE per
 // gnnstage_workspace_size / gnnstage_create call (both must see the same values) and the result is kept in

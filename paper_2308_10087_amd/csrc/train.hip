@@ -20,7 +20,7 @@ namespace {
 constexpr int kMaxSplits = 256;  // split-reduction scratch of the weight-gradient product
 constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;
 
-std::string g_create_error;
+thread_local std::string g_create_error;  // of calls without a handle: threads may be refused at once
 
 inline uint64_t splitmix64(uint64_t z) {
   z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;

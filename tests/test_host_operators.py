@@ -113,3 +113,23 @@ def test_tensors_are_checked_before_anything_else():
         with pytest.raises(g.GnnStageError) as e:
             call()
         assert e.value.code == -1, i
+
+
+def test_refusals_of_threads_keep_apart():
+    """A message is the calling thread's: another one's refusal neither replaces nor frees it."""
+    import threading
+    assert _head(d=0) == -1 and _store(ld_x=99) == -1
+    mine = lib.gnntrain_last_error(None), lib.gnnstage_last_error(None)
+    others = []
+
+    def refused():
+        before = lib.gnntrain_last_error(None), lib.gnnstage_last_error(None)
+        assert _head(ld_h=63) == -1 and _store(rows=-1) == -1
+        others.append((before, (lib.gnntrain_last_error(None), lib.gnnstage_last_error(None))))
+
+    t = threading.Thread(target=refused)
+    t.start()
+    t.join()
+    assert (lib.gnntrain_last_error(None), lib.gnnstage_last_error(None)) == mine
+    (before, after), = others
+    assert before == (b"", b"") and b"leading dimension" in after[0] and b"rows" in after[1]
