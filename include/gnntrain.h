@@ -70,8 +70,10 @@ typedef struct {
                            come from gnnstage_level_buffers */
   void *workspace;    /* DEVICE, 256-byte aligned, >= gnntrain_workspace_size() bytes */
   size_t workspace_bytes;
-  int32_t head_fused; /* non-zero: the head is gnntrain_head_xent, which keeps neither logits nor their gradients; n_classes may then be up to
-                         2^24 (otherwise 65,536) */
+  int32_t head_fused; /* non-zero: the head is gnntrain_head_xent, which keeps neither logits nor their gradients of all vertices; n_classes may then be up to
+                         2^24 (otherwise 65,536).  Takes less memory from about 16 classes on where the last level is bf16 and 64, 128 or 256 wide (its rows are read in
+                         place); otherwise packed rows are kept, of up to 2^20 vertices (fp32, or wider than 256: 131,072, with fp32 sums and logits), and it is the
+                         classes beyond a row's width that make it smaller: 89,250 x 100 fp32, 7 classes 78 MB for 6 */
 } gnntrain_desc;
 
 /* Device bytes the loop needs: optimiser moments, logits of up to 131,072 vertices, gradient of the logits and
@@ -115,7 +117,8 @@ int gnntrain_softmax_xent(const float *logits, int32_t ld, const float *bias, co
                           int32_t dl_dtype, int32_t dl_ld, float *row_loss, void *hip_stream);
 
 /* The loss head over many classes: what a linear classifier, gnntrain_softmax_xent and the classifier's gradients compute, without
- * the logits of all rows and classes in memory at any time.  z = h_r W + bias; for a labelled row: row_loss = log sum_c
+ * the logits of all rows and classes in memory: those of bf16 rows of up to 256 columns never leave the registers, of others at most 2^26 are there at a time,
+ * with their gradients.  z = h_r W + bias; for a labelled row: row_loss = log sum_c
  * exp(z_c) - z_label, g_c = (softmax_c - [c = label]) * inv_n_train; dh = g W^T, dW += h^T g, db += column sums of g.  A row is
  * labelled when mask (NULL: all rows) is non-zero and its label is in [0, n_classes); any other row has loss 0 and a zero row of
  * dh, takes no part in dW and db whatever it holds, and may hold anything.

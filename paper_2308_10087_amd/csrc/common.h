@@ -451,6 +451,10 @@ int tn32_splits(int64_t M, int I, int O);
 int launch_tn32(const float *A, int64_t lda, const float *B, int64_t ldb, int M, int I, int O, float *D, int64_t ldd, float *sums, float *part,
                 float *part_sum, int max_splits, hipStream_t s);
 
+// What gnntrain_head_xent needs at least for all gradients of rows that are where they are: gnntrain_head_xent_workspace_size() less the room for a packed copy that
+// they do not need.  0: the sizes are refused (train_error() has been told why).
+size_t head_workspace_bytes(const void *h, int64_t ld_h, int64_t rows, int d, int n_classes, int dtype);
+
 // ---- rows in 8 bits -----------------------------------------------------------------------------
 // q (16-byte aligned, ld_q a multiple of 16 and at least d rounded up to 32, written up to there) and scale (a byte per 32 columns) from
 // rows of any alignment

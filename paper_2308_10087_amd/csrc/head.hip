@@ -1000,14 +1000,21 @@ struct ClassesArgs {
   int32_t C, d, class_tiles;
   float inv_n;
   float *dW, *db;          // "+=", either may be NULL
-  float *part;             // [group][2][DP][kOwned]
-  float *part_db;          // [group][2][kOwned]
+  float *part;             // [slot][DP][part_cols]
+  float *part_db;          // [slot][kOwned]
+  int32_t part_cols;       // kOwned, or a single class tile's columns in whole waves
+  int32_t by_tile;         // which slots, see slot_of
 };
 // The classes kernel's work, (class tile, row step) pairs in that order, is cut into one run per workgroup (group g: from pair
 // total g / groups on), so that all of them end together: with a workgroup per class tile, 782 class tiles in rounds of 512 took 2.88 ms.  A run's
-// class tiles that are whole are added to dW and db by the kernel; of one that is cut, a group writes its share, in its first slot if
-// its run begins in that tile and in its second if it does not.
+// class tiles that are whole are added to dW and db by the kernel; of one that is cut, a group writes its share.
 __device__ inline int64_t run_begin(int64_t total, int groups, int g) { return total * g / groups; }
+// Where: a run has two cut tiles at most, the one that it begins in and the one that it ends in.  And from share to share group or tile go up by one, never down, so
+// that their sum is a place of its own too: with few class tiles that is half the room (232,965 rows x 256, 41 classes: 34 MB, 134 MB with two slots a group
+// of 128 columns each).
+__device__ inline int64_t slot_of(const ClassesArgs &a, int group, int class_tile, bool begins) {
+  return a.by_tile ? (int64_t)group + class_tile : 2 * (int64_t)group + (begins ? 0 : 1);
+}
 
 //
 // EXACT: 16 bits of g are up to 2^-16 of a single term of dW.  Added up over many labelled rows of a class that is less than what an fp32 product's own sum is off by;
@@ -1156,7 +1163,7 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_classes_kernel(const C
       if (tile + 1 < end) step(tile + 1, (const lds_char *)tile1, &stats1, (lds_char *)tile0, &stats0);
     }
     const bool whole = begin == 0 && end == row_steps;
-    const int64_t slot = 2 * (int64_t)group + (pair == run0 ? 0 : 1);
+    const int64_t slot = slot_of(a, group, class_tile, pair == run0);
     pair += end - begin;
     if (c >= a.C) continue;
     g_sum += __shfl_xor(g_sum, 32);
@@ -1167,8 +1174,8 @@ __global__ __launch_bounds__(256, kPerUnit<DP>) void head_classes_kernel(const C
         a.part_db[slot * kOwned + wave * 32 + (lane & 31)] = g_sum;
     }
     if (a.dW == nullptr) continue;
-    float *to = whole ? a.dW + c : a.part + slot * DP * kOwned + wave * 32 + (lane & 31);
-    int64_t stride = whole ? a.C : kOwned;
+    float *to = whole ? a.dW + c : a.part + slot * DP * a.part_cols + wave * 32 + (lane & 31);
+    int64_t stride = whole ? a.C : a.part_cols;
     const int d = DIRECT ? DP : a.d;
     asm volatile("" : "+s"(stride));  // (or the compiler makes all addresses ahead of the loop, and spills)
     to += 4 * h * stride;
@@ -1218,10 +1225,10 @@ __global__ __launch_bounds__(256) void head_reduce_kernel(const ClassesArgs a) {
   };
   const int g0 = owner(from), g1 = owner(to - 1);
   if (g0 == g1) return;  // whole workgroup: nothing was cut
-  const int first_slot = run_begin(total, groups, g0) >= from ? 0 : 1;
+  const bool begins = run_begin(total, groups, g0) >= from;  // the first of them, in this tile
   auto share = [&](int k, int g) {
-    const int64_t slot = 2 * (int64_t)g + (g == g0 ? first_slot : 0);
-    return k == a.d ? a.part_db[slot * kOwned + in_tile] : a.part[(slot * DP + k) * kOwned + in_tile];
+    const int64_t slot = slot_of(a, g, class_tile, g != g0 || begins);
+    return k == a.d ? a.part_db[slot * kOwned + in_tile] : a.part[(slot * DP + k) * a.part_cols + in_tile];
   };
   auto wanted = [&](int k) { return k < a.d ? a.dW != nullptr : k == a.d && a.db != nullptr; };
   auto add = [&](int k, float x) {
@@ -1399,14 +1406,20 @@ __global__ __launch_bounds__(256) void head_pack_kernel(const PrepareArgs a) {
 
 struct FusedPlan {
   int64_t rows = 0, padded_rows = 0, max_items = 0;
-  int d = 0, C = 0, DP = 0, padded_classes = 0, n_counts = 0, max_splits = 1, class_tiles = 0;
+  int d = 0, C = 0, DP = 0, padded_classes = 0, n_counts = 0, max_splits = 1, class_tiles = 0, part_cols = kOwned;
+  bool by_tile = false;
   size_t counts = 0, meta = 0, list = 0, stats = 0, packed = 0, Wt = 0, bias = 0, part = 0, part_stat = 0, part_dW = 0, part_db = 0, total = 0;
 };
 constexpr int64_t kFusedRows = (int64_t)1 << 20;  // of a slab: their packed copy is half a gigabyte at most
 
 bool fused_takes(int d, int dtype) { return dtype == GNNSTAGE_BF16 && d <= 256; }
 
-FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads) {
+// Rows of the very width in whole 16-byte pieces are read where they are, others from a packed copy.
+bool read_in_place(const void *h, int64_t ld_h, int d) {
+  return (d == 64 || d == 128 || d == 256) && ld_h % 8 == 0 && (reinterpret_cast<uintptr_t>(h) & 15u) == 0;
+}
+
+FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads, bool in_place) {
   FusedPlan p;
   const int64_t rows = std::min(all_rows, kFusedRows);
   p.rows = rows;
@@ -1431,17 +1444,20 @@ FusedPlan fused_plan(int64_t all_rows, int d, int C, bool grads) {
   p.meta = take(sizeof(Meta));
   p.list = take(sizeof(int32_t) * (size_t)p.padded_rows);
   p.stats = take(4 * sizeof(float) * (size_t)p.padded_rows);
-  // (also where the rows can be read as they are: whether they can is not known from their sizes)
-  p.packed = take(2 * (size_t)p.padded_rows * p.DP);
   p.Wt = take(2 * (size_t)p.padded_classes * p.DP);
   p.bias = take(sizeof(float) * (size_t)p.padded_classes);
   const int64_t part_items = p.max_splits > 1 ? std::min<int64_t>(p.max_items, kRowItems) : 0;
   p.part_stat = take(sizeof(float) * 4 * kOwned * (size_t)part_items);
   p.part = take(grads ? sizeof(float) * (size_t)kOwned * p.DP * (size_t)part_items : 0);
   const int64_t groups = grads ? std::min<int64_t>(round_of(p.DP), ((int64_t)p.class_tiles * ((rows + kTile - 1) / kTile) + 3) / 4) : 0;
-  p.part_dW = take(sizeof(float) * 2 * (size_t)groups * p.DP * kOwned);
-  p.part_db = take(sizeof(float) * 2 * (size_t)groups * kOwned);
-  p.total = off;
+  p.by_tile = p.class_tiles < groups;
+  p.part_cols = p.class_tiles == 1 ? round_up(C, 32) : kOwned;
+  const int64_t slots = p.by_tile ? groups + p.class_tiles : 2 * groups;
+  p.part_dW = take(sizeof(float) * (size_t)slots * p.DP * p.part_cols);
+  p.part_db = take(sizeof(float) * (size_t)slots * kOwned);
+  // last, so that a call whose rows need no copy can do without
+  p.packed = off;
+  p.total = align256(off + (in_place ? 0 : 2 * (size_t)p.padded_rows * p.DP));
   return p;
 }
 
@@ -1542,6 +1558,8 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
   k.db = c.db;
   k.part = reinterpret_cast<float *>(at(p.part_dW));
   k.part_db = reinterpret_cast<float *>(at(p.part_db));
+  k.part_cols = p.part_cols;
+  k.by_tile = p.by_tile;
   const int64_t groups = std::max<int64_t>(round_of(p.DP), p.class_tiles);  // at most
   hipLaunchKernelGGL((head_classes_kernel<DP, DIRECT, true, kClassesInRegs<DP>>), dim3((unsigned)groups), dim3(256), 0, s, k);
   HEAD_TRY(hipGetLastError());
@@ -1556,16 +1574,24 @@ int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipSt
 }
 template <int DP>
 int run_fused(const FusedPlan &p, const Call &c, int64_t rows, bool first, hipStream_t s) {
-  // rows of the very width in whole 16-byte pieces are read where they are, others from a packed copy
-  const bool direct = p.d == DP && c.ld_h % 8 == 0 && (reinterpret_cast<uintptr_t>(c.h) & 15u) == 0;
-  return direct ? run_fused<DP, true>(p, c, rows, first, s) : run_fused<DP, false>(p, c, rows, first, s);
+  return read_in_place(c.h, c.ld_h, p.d) ? run_fused<DP, true>(p, c, rows, first, s) : run_fused<DP, false>(p, c, rows, first, s);
 }
 
-size_t workspace_bytes_of(const Plan &p) {
-  return fused_takes(p.d, p.dtype) ? fused_plan(p.rows, p.d, p.C, p.grads).total : p.total;
+size_t workspace_bytes_of(const Plan &p, bool in_place) {
+  return fused_takes(p.d, p.dtype) ? fused_plan(p.rows, p.d, p.C, p.grads, in_place).total : p.total;
 }
 
 }  // namespace
+
+size_t head_workspace_bytes(const void *h, int64_t ld_h, int64_t rows, int d, int n_classes, int dtype) {
+  Plan p;
+  std::string err;
+  if (!make_plan(rows, d, n_classes, dtype, true, p, err)) {
+    train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: " + err);
+    return 0;
+  }
+  return workspace_bytes_of(p, read_in_place(h, ld_h, d));
+}
 
 extern "C" size_t gnntrain_head_xent_workspace_size(int64_t rows, int32_t d, int32_t n_classes, int32_t dtype, int32_t want_grads) try {
   Plan p;
@@ -1574,7 +1600,7 @@ extern "C" size_t gnntrain_head_xent_workspace_size(int64_t rows, int32_t d, int
     train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: " + err);
     return 0;
   }
-  return workspace_bytes_of(p);
+  return workspace_bytes_of(p, false);  // whether rows can be read in place is not known from their sizes
 }
 GNNSTAGE_GUARD_SIZE
 
@@ -1590,12 +1616,12 @@ extern "C" int gnntrain_head_xent(const void *h, int64_t ld_h, const void *W, in
   if (!h || !W || !labels || !row_loss) return train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: h, W, labels and row_loss must not be NULL");
   if (dh == h) return train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: dh must not be h, which is read after dh is written");
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return train_error(GNNSTAGE_EINVAL, "gnntrain_head_xent: workspace must be 256-byte aligned");
-  if (workspace_bytes < workspace_bytes_of(p)) return train_error(GNNSTAGE_ENOMEM, "gnntrain_head_xent: workspace smaller than gnntrain_head_xent_workspace_size()");
+  if (workspace_bytes < workspace_bytes_of(p, read_in_place(h, ld_h, d))) return train_error(GNNSTAGE_ENOMEM, "gnntrain_head_xent: workspace smaller than gnntrain_head_xent_workspace_size()");
   const Call c{h, ld_h, W, bias, labels, mask, inv_n_train, row_loss, dh, ld_dh, dW, db, static_cast<char *>(workspace)};
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   int e = hipSuccess;
   if (fused_takes(d, dtype)) {
-    const FusedPlan f = fused_plan(rows, d, n_classes, grads);
+    const FusedPlan f = fused_plan(rows, d, n_classes, grads, read_in_place(h, ld_h, d));
     for (int64_t r = 0; r < rows && e == hipSuccess; r += f.rows) {
       Call slab = c;
       slab.h = static_cast<const bf16_t *>(h) + (size_t)(r * ld_h);

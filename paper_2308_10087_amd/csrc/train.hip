@@ -229,7 +229,7 @@ bool read_dims(const gnntrain_desc *d, Dims &x, std::string &err) {
   x.Kp = round_up(x.d_top, 8);
   x.head_rows = std::min<int64_t>(x.n, 131072);
   if (x.fused) {
-    x.head_bytes = gnntrain_head_xent_workspace_size(x.n, x.d_top, x.C, x.dtype, 1);
+    x.head_bytes = head_workspace_bytes(gnnstage_buffer(last, GNNSTAGE_B_CUR, L), x.d_top, x.n, x.d_top, x.C, x.dtype);
     if (x.head_bytes == 0) { err = gnntrain_last_error(nullptr); return false; }  // its own limits: of the last level's width, of the weights
   }
   x.n_param_elems = 0;

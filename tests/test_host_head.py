@@ -27,18 +27,20 @@ def _child(runtime, what, *args):
 
 
 # ---- in the child -----------------------------------------------------------------------------------------------
-def _trainer(rt, d_top, n_classes, bf16, fused):
+def _trainer(rt, d_top, n_classes, bf16, fused, n=60):
     """Workspace size, message, what gnntrain_create returns and its message, for a stage whose last level is d_top wide."""
     from test_host_launches import _Stage
 
     from paper_2308_10087_amd.binding import gnntrain_desc, lib
-    st = _Stage("gcn", [8, d_top], 2, n=60, bf16=bf16)
+    st = _Stage("gcn", [8, d_top], 2, n=n, bf16=bf16)
     some = np.zeros(4096, np.uint8)
     at = (some.ctypes.data + 255) // 256 * 256
     d = gnntrain_desc()
     hs = (C.c_void_p * 1)(st.h)
     d.n_stages, d.stages, d.n_classes = 1, C.cast(hs, C.c_void_p), n_classes
-    d.head_W = d.head_b = d.head_dW = d.head_db = d.labels = at
+    labels = np.zeros(n, np.int32)
+    d.head_W = d.head_b = d.head_dW = d.head_db = at
+    d.labels = labels.ctypes.data
     d.optimizer, d.alpha_hist, d.head_fused = 0, 1, fused
     size = lib.gnntrain_workspace_size(C.byref(d))
     why = lib.gnntrain_last_error(None).decode()
@@ -129,3 +131,11 @@ def test_heads_at_their_limits_can_be_launched(runtime):
              for bf16 in (0, 1) for grads in (0, 1)]
     for c, (size, rc, why, launches) in zip(cases, _child(runtime, "_each", "_head", cases)):
         assert size > 0 and rc == 0 and launches > 0, (c, why)
+
+
+@pytest.mark.parametrize("n,d_top,n_classes", [(232965, 256, 41), (169343, 128, 40), (700001, 128, 47), (46657, 256, 10007), (46657, 64, 16)])
+def test_a_loop_without_logits_needs_no_more_memory(runtime, n, d_top, n_classes):
+    """bf16 levels of a width that is read in place: the head without logits in the place of the one that keeps them, from 16 classes on."""
+    fused = _child(runtime, "_trainer", d_top, n_classes, True, 1, n)
+    kept = _child(runtime, "_trainer", d_top, n_classes, True, 0, n)
+    assert fused[2] == kept[2] == 0 and 0 < fused[0] <= kept[0], (fused[0], kept[0])
