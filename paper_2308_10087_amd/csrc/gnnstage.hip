@@ -548,8 +548,8 @@ bool read_shape(const gnnstage_desc *d, Shape &s, std::string &err) {
 }
 
 // Saved aggregations in 8 bits.  A layer's aggregation is then needed as it is by the layer's own transform alone: it borrows
-// rows that only the backward pass uses, the widest of the gradient rows (dZ of any layer); where no layer's are wide enough it gets room
-// of its own, one for all layers.
+// rows that only the backward pass uses, the widest of the gradient rows (dZ or, outside of ResGCN+ where they share a table with the forward pass, dY of any
+// layer); where no layer's are wide enough it gets room of its own, one for all layers.
 void save_in_8_bits(const Shape &s, Layout &l, Bump &w) {
   l.Z8.assign(s.L, 0);
   l.Z8s.assign(s.L, 0);
@@ -561,6 +561,10 @@ void save_in_8_bits(const Shape &s, Layout &l, Bump &w) {
     if (there && ld > width) {
       width = ld;
       at = l.dZ[j];
+    }
+    if (!s.res() && !s.tf[j] && s.defer_wgrad() && s.ld[j + 1] > width) {
+      width = s.ld[j + 1];
+      at = l.dY[j];
     }
     if (!s.tf[j]) need = std::max(need, s.ld[j]);
   }

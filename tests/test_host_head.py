@@ -80,6 +80,30 @@ def _head(rt, rows, d, n_classes, bf16, grads):
     return [size, rc, lib.gnntrain_last_error(None).decode() if rc else "", rt.host_launches()]
 
 
+def _save8_sizes(rt, variant, dims, bf16, need_input_grad, n):
+    """Workspace of a stage without save_8bit and with."""
+    from test_host_launches import _Stage
+
+    from paper_2308_10087_amd import binding
+    real, seen = binding.lib, []
+
+    class Listening:
+        def __getattr__(self, name):
+            if name == "gnnstage_workspace_size":
+                return lambda d: (seen.append(d._obj), real.gnnstage_workspace_size(d))[1]
+            return getattr(real, name)
+
+    binding.lib = Listening()
+    stage = _Stage(variant, dims, 4, n=n, bf16=bool(bf16))
+    binding.lib = real
+    d = seen[0]
+    d.need_input_grad = need_input_grad
+    sizes = []
+    for d.save_8bit in (0, 1):
+        sizes.append(real.gnnstage_workspace_size(C.byref(d)))
+    return sizes
+
+
 if __name__ == "__main__":
     _rt = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
     from test_host_launches import _Launch
@@ -139,3 +163,12 @@ def test_a_loop_without_logits_needs_no_more_memory(runtime, n, d_top, n_classes
     fused = _child(runtime, "_trainer", d_top, n_classes, True, 1, n)
     kept = _child(runtime, "_trainer", d_top, n_classes, True, 0, n)
     assert fused[2] == kept[2] == 0 and 0 < fused[0] <= kept[0], (fused[0], kept[0])
+
+
+def test_saved_rows_in_8_bits_never_take_more_room(runtime):
+    """Layers that aggregate first are as wide as their input at most where they write, so the backward pass has rows for an aggregation to borrow, also without a
+    gradient of the input."""
+    cases = [(v, dims, bf16, grad, 4000) for v, dims in [("gcn", [128, 128]), ("gcn", [256, 256]), ("gcn", [100, 256, 46]), ("gcn", [34, 64, 64]), ("sage", [128, 128]),
+                                                         ("sage", [64, 100, 100]), ("resgcn", [64, 64, 64])] for bf16 in (0, 1) for grad in (0, 1)]
+    for c, (plain, small) in zip(cases, _child(runtime, "_each", "_save8_sizes", cases)):
+        assert 0 < small < plain, (c, plain, small)
