@@ -173,3 +173,19 @@ def test_norms_over_many_classes(rows, d, C, dtype):
 def test_weight_gradients_of_classes_with_many_rows(d):
     """More than 16,384 labelled rows and more than 128 a class: two bf16 numbers of every g, of rows as they are and packed."""
     check_head(34000, d, 100, "bf16", "some")
+
+
+@pytest.mark.parametrize("d,C,pad", [(8, 3, 0), (64, 5, 8)])
+def test_more_rows_than_a_slab(d, C, pad):
+    """2^20 rows go at a time: weights and biases of the first slab serve the next, whose labels, mask, losses and gradient rows begin further on, and whose sums are
+    added to the first one's.  Labelled rows on both sides of the border."""
+    rows = (1 << 20) + 129
+
+    def edit(h, W, b, y, mask):
+        mask[(1 << 20) - 3:(1 << 20) + 5] = 1
+        y[(1 << 20) - 3:(1 << 20) + 5] = np.arange(8) % C
+        mask[-1], y[-1] = 1, C - 1
+
+    got = check_head(rows, d, C, "bf16", "some", pad=pad, edit=edit)
+    border = slice((1 << 20) - 3, (1 << 20) + 5)
+    assert np.all(got["loss"][border] > 0) and np.all(np.abs(got["dh"][border]).max(1) > 0) and got["loss"][-1] > 0
