@@ -139,7 +139,8 @@ typedef struct {
                       GNNSTAGE_SAGE: on every layer's output; GNNSTAGE_GCNII: must be 0 */
   int32_t save_8bit; /* non-zero: what the forward pass saves for the weight gradients (the aggregations of layers that aggregate
                         first, gnnstage_layer_order) is kept in 8 bits, see gnnstage_rows8_store.  Levels and gradients of rows are the same bits
-                        as without, bias gradients the same sums (bf16: in another order); weight gradients are those of the stored values */
+                        as without, bias gradients the same sums (bf16: in another order); weight gradients are those of the stored values.  The workspace
+                        shrinks by what is saved, unless every layer writes rows narrower than it aggregates (the aggregations then take room of their own) */
 } gnnstage_desc;
 
 /* Device bytes the stage needs inside desc->workspace (graph tables, transposed index,
