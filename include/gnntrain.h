@@ -33,7 +33,7 @@ extern "C" {
 
 typedef struct gnntrain gnntrain_t; /* opaque, owned by the library */
 
-enum { GNNTRAIN_SGD = 0, GNNTRAIN_ADAM = 1 };
+enum { GNNTRAIN_SGD = 0, GNNTRAIN_ADAM = 1, GNNTRAIN_ADAMW = 2 };
 
 /* One trainable tensor.  The optimiser works on the fp32 master copy; after every step it also writes the
  * copy the kernels read when that is a different buffer (bf16 stages: W[j] of gnnstage_desc, head_W). */
@@ -59,7 +59,8 @@ typedef struct {
   /* parameters of all stages and of the head, in the order they are stepped */
   int32_t n_params;
   const gnntrain_param *params; /* HOST array */
-  int32_t optimizer;            /* GNNTRAIN_SGD: p -= lr (g + wd p);  GNNTRAIN_ADAM: Kingma & Ba, Algorithm 1 */
+  int32_t optimizer;            /* GNNTRAIN_SGD: p -= lr (g + wd p);  GNNTRAIN_ADAM: Kingma & Ba, Algorithm 1 (wd p is added to g);
+                                   GNNTRAIN_ADAMW: gnntrain_adamw_step (wd apart from g; buffers of parameters may then not overlap) */
   float lr, beta1, beta2, eps, weight_decay;
   int32_t shuffle;    /* 0: chunks in index order every epoch */
   uint64_t seed;      /* of the chunk shuffling, and of the dropout decisions of stages that have dropout: stage s
@@ -74,6 +75,8 @@ typedef struct {
                          2^24 (otherwise 65,536).  Takes less memory from about 16 classes on where the last level is bf16 and 64, 128 or 256 wide (its rows are read in
                          place); otherwise packed rows are kept, of up to 2^20 vertices (fp32, or wider than 256: 131,072, with fp32 sums and logits), and it is the
                          classes beyond a row's width that make it smaller: 89,250 x 100 fp32, 7 classes 78 MB for 6 */
+  int32_t state_8bit;  /* GNNTRAIN_ADAMW: non-zero keeps its states in 8 bits (2.06 bytes per parameter of the workspace instead of 8; draws from seed).
+                          Must be zero with another optimizer */
 } gnntrain_desc;
 
 /* Device bytes the loop needs: optimiser moments, logits of up to 131,072 vertices, gradient of the logits and
@@ -156,6 +159,35 @@ int gnntrain_sum_static(const float *x, int64_t n, float scale, float *out, void
 int gnntrain_adam_step(float *p, const float *g, float *m, float *v, void *compute, int32_t compute_dtype,
                        int64_t count, float lr, float beta1, float beta2, float eps, float weight_decay, int64_t t,
                        void *hip_stream);
+/* One AdamW step (Loshchilov & Hutter, ICLR 2019, Algorithm 2) over all tensors of a model at once:
+ *   g' = grad_scale g;  m = beta1 m + (1 - beta1) g';  v = beta2 v + (1 - beta2) g'^2;
+ *   p = p (1 - lr weight_decay) - lr c1 m / (sqrt(c2 v) + eps),  c = 1 / (1 - beta^t);  compute = p, rounded
+ * state_bits 32: m and v are fp32.  state_bits 8: m and the root of v are kept in blocks of 32 elements, a factor 2^e each (the byte e + 127 in
+ * m_scale / v_scale, (count + 31) / 32 bytes) and a byte per element, the finite numbers of OCP's e4m3 (MXFP8): a value is rounded to one of its two
+ * neighbours, at most 1/8 of itself apart from 2^-14 of the block's largest value on, by a draw that keeps the mean (nearest rounding would not: a step moves v by 1 - beta2 of
+ * itself); what is above zero in v stays so.  All bytes zero are states of zero.  A block with a NaN, an infinity or 2^127 among its values is all NaN (byte 255).
+ * The draws come from seed, t, the tensor's place in the list and the element's in the tensor (see SplitMix64 at gnntrain_chunk_order): with o(x) the
+ * generator's output for state x, gamma its constant, tensor k has the key o(o(seed + t gamma) + (k + 1) gamma), its elements 2 j and 2 j + 1 the low and high half of
+ * o(key + (j + 1) gamma), of which the low 16 bits are m's and the high ones v's.  The same call gives the same bits.
+ * tensors: HOST, n of them, read during the call.  p (fp32), g (of g_dtype), compute (of compute_dtype, or NULL, or p): DEVICE, count elements, at any multiple of
+ * their elements' size; m, v: DEVICE, count floats or bytes, at multiples of four bytes.  Buffers that are written may not overlap any other (gradients may
+ * be shared).  count in [0, 2^35].  t = 1, 2, ...: a host number, as lr is, so that a captured call repeats its step.  grad_scale: DEVICE, one
+ * float (what clips the gradients' norm, say), or NULL: 1.  beta1, beta2 in [0, 1).  Asynchronous, needs no workspace.
+ * Message of an error: gnntrain_last_error(NULL). */
+typedef struct {
+  float *p;
+  const void *g;
+  int32_t g_dtype;       /* GNNSTAGE_F32 or GNNSTAGE_BF16 */
+  int32_t compute_dtype; /* the same; read only with compute */
+  void *compute;
+  void *m, *v;
+  uint8_t *m_scale, *v_scale; /* state_bits 8 */
+  int64_t count;
+  float weight_decay;
+} gnntrain_adamw_tensor;
+int gnntrain_adamw_step(const gnntrain_adamw_tensor *tensors, int32_t n, int32_t state_bits, float lr, float beta1, float beta2, float eps,
+                        const float *grad_scale, int64_t t, uint64_t seed, void *hip_stream);
+
 int gnntrain_sgd_step(float *p, const float *g, void *compute, int32_t compute_dtype, int64_t count, float lr,
                       float weight_decay, void *hip_stream);
 

@@ -57,8 +57,14 @@ class gnntrain_desc(C.Structure):
         ("optimizer", C.c_int32), ("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
         ("weight_decay", C.c_float),
         ("shuffle", C.c_int32), ("seed", C.c_uint64), ("alpha_hist", C.c_int32), ("history_swap", C.c_int32),
-        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("head_fused", C.c_int32),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("head_fused", C.c_int32), ("state_8bit", C.c_int32),
     ]
+
+
+class gnntrain_adamw_tensor(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("g_dtype", C.c_int32), ("compute_dtype", C.c_int32), ("compute", C.c_void_p),
+                ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("count", C.c_int64),
+                ("weight_decay", C.c_float)]
 
 
 def _load():
@@ -174,6 +180,9 @@ def _load():
     lib.gnntrain_sgd_step.restype = C.c_int
     lib.gnntrain_sgd_step.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_float,
                                       C.c_void_p]
+    lib.gnntrain_adamw_step.restype = C.c_int
+    lib.gnntrain_adamw_step.argtypes = [C.POINTER(gnntrain_adamw_tensor), C.c_int32, C.c_int32, C.c_float, C.c_float, C.c_float, C.c_float, C.c_void_p,
+                                        C.c_int64, C.c_uint64, C.c_void_p]
     lib.gnntrain_head_xent_workspace_size.restype = C.c_size_t
     lib.gnntrain_head_xent_workspace_size.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
     lib.gnntrain_head_xent.restype = C.c_int
@@ -677,7 +686,7 @@ class GnnStage:
 
 
 # ---- training loop (include/gnntrain.h) -------------------------------------------------------
-GNNTRAIN_SGD, GNNTRAIN_ADAM = 0, 1
+GNNTRAIN_SGD, GNNTRAIN_ADAM, GNNTRAIN_ADAMW = 0, 1, 2
 
 
 def _cur_stream():
@@ -777,14 +786,74 @@ def gnntrain_sgd_step(p, g, compute, lr, weight_decay) -> None:
         raise GnnStageError(rc, "gnntrain_sgd_step")
 
 
+class AdamwTensors:
+    """What gnntrain_adamw_step goes through: the C list, made once, and the tensors that it points at."""
+
+    def __init__(self, array, bits, device, keep):
+        self.array, self.bits, self.device, self._keep = array, bits, device, keep
+
+
+def gnntrain_adamw_tensors(tensors) -> AdamwTensors:
+    """A model's list for gnntrain_adamw_step.  A tensor is a dict: ``p`` fp32; ``g`` fp32 or bf16; ``m``, ``v`` fp32, or uint8 codes with ``m_scale``,
+    ``v_scale`` uint8 [(elements + 31) / 32] (the same for all tensors); ``compute`` fp32 or bf16, or None; ``weight_decay``.  Of any shape, contiguous, the codes at
+    multiples of four bytes."""
+    import torch
+    name = "gnntrain_adamw_tensors"
+    array = (gnntrain_adamw_tensor * max(len(tensors), 1))()
+    bits, device, keep = None, None, []
+    for i, x in enumerate(tensors):
+        unknown = set(x) - {"p", "g", "m", "v", "m_scale", "v_scale", "compute", "weight_decay"}
+        if unknown or not {"p", "g", "m", "v"} <= set(x):
+            _refuse(name, f"tensor {i} needs p, g, m and v, and has {sorted(x)}")
+        p, g, m, v, compute = x["p"], x["g"], x["m"], x["v"], x.get("compute")
+        device = p.device if device is None else device
+        mine = 8 if m.dtype == torch.uint8 else 32
+        if bits not in (None, mine):
+            _refuse(name, "all states must be of the same type")
+        bits, n = mine, p.numel()
+        state = torch.uint8 if bits == 8 else torch.float32
+        _tensor(name, f"p of tensor {i}", p, p.shape, torch.float32, device)
+        for what, t, dtype in (("g", g, g.dtype), ("m", m, state), ("v", v, state)) + ((("compute", compute, compute.dtype),) if compute is not None else ()):
+            _tensor(name, f"{what} of tensor {i}", t, p.shape, dtype, device)
+        a = array[i]
+        a.p, a.g, a.m, a.v, a.count = p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), n
+        a.g_dtype = _dtype_code(name, f"g of tensor {i}", g)
+        a.compute, a.compute_dtype = (None, GNNSTAGE_F32) if compute is None else (compute.data_ptr(), _dtype_code(name, f"compute of tensor {i}", compute))
+        scales = [x.get("m_scale"), x.get("v_scale")]
+        if bits == 8:
+            for what, t in zip(("m_scale", "v_scale"), scales):
+                if t is None:
+                    _refuse(name, f"states in 8 bits need {what}")
+                _tensor(name, f"{what} of tensor {i}", t, ((n + 31) // 32,), torch.uint8, device)
+            a.m_scale, a.v_scale = scales[0].data_ptr(), scales[1].data_ptr()
+        a.weight_decay = float(x.get("weight_decay", 0.0))
+        keep.append((p, g, m, v, compute, scales))
+    return AdamwTensors(array, bits or 32, device, keep)
+
+
+def gnntrain_adamw_step(tensors: AdamwTensors, lr, beta1, beta2, eps, t, seed: int = 0, grad_scale=None) -> None:
+    """One AdamW step over all of them (t = 1, 2, ...); grad_scale: fp32 tensor of one element that the gradients are multiplied by, or None."""
+    import torch
+    name = "gnntrain_adamw_step"
+    n = len(tensors._keep)
+    if n == 0:
+        return
+    if grad_scale is not None:
+        _tensor(name, "grad_scale", grad_scale.reshape(-1), (1,), torch.float32, tensors.device)
+    rc = _launch(name, tensors.device, lib.gnntrain_adamw_step, tensors.array, n, tensors.bits, float(lr), float(beta1), float(beta2), float(eps),
+                 None if grad_scale is None else grad_scale.data_ptr(), int(t), int(seed) & ((1 << 64) - 1))
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnntrain_last_error(None).decode())
+
+
 class GnnTrainer:
     """Handle of the epoch loop plus the tensors it points at.  ``params`` is a list of
     ``(master fp32 tensor, compute tensor or None, grad fp32 tensor)``.  ``head_fused``: the loss head keeps no logits
-    (gnntrain_head_xent)."""
+    (gnntrain_head_xent).  ``state_8bit``: GNNTRAIN_ADAMW keeps its states in 8 bits."""
 
     def __init__(self, stages: Sequence["GnnStage"], *, head_W, head_b, head_dW, head_db, labels, train_mask, params,
                  optimizer=GNNTRAIN_ADAM, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, shuffle=True,
-                 seed=0, alpha_hist=1, history_swap=False, device="cuda:0", head_fused=False):
+                 seed=0, alpha_hist=1, history_swap=False, device="cuda:0", head_fused=False, state_8bit=False):
         import torch
 
         self._torch = torch
@@ -811,6 +880,7 @@ class GnnTrainer:
         d.shuffle, d.seed, d.alpha_hist = int(bool(shuffle)), int(seed), int(alpha_hist)
         d.history_swap = int(bool(history_swap))
         d.head_fused = int(bool(head_fused))
+        d.state_8bit = int(bool(state_8bit))
         size = int(lib.gnntrain_workspace_size(C.byref(d)))
         if size == 0:
             raise GnnStageError(-1, "gnntrain_workspace_size: " + lib.gnntrain_last_error(None).decode())

@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/gnntrain.h"
+#include "adamw.h"
 #include "common.h"
 
 namespace {
@@ -193,7 +194,7 @@ UpdateArgs adam_args(float lr, float b1, float b2, float eps, float wd, int64_t 
 }
 
 struct Layout {
-  size_t m = 0, v = 0, logits = 0, dlogits = 0, dtop = 0, row_loss = 0, scratch = 0, loss = 0, Wt = 0, Wn = 0, gemm_partial = 0,
+  size_t m = 0, v = 0, m_scale = 0, v_scale = 0, logits = 0, dlogits = 0, dtop = 0, row_loss = 0, scratch = 0, loss = 0, Wt = 0, Wn = 0, gemm_partial = 0,
          bias_partial = 0, head = 0, total = 0;
 };
 
@@ -215,7 +216,8 @@ bool read_dims(const gnntrain_desc *d, Dims &x, std::string &err) {
     return false;
   }
   if (d->n_params < 0 || (d->n_params > 0 && !d->params)) { err = "params is NULL"; return false; }
-  if (d->optimizer != GNNTRAIN_SGD && d->optimizer != GNNTRAIN_ADAM) { err = "unknown optimizer"; return false; }
+  if (d->optimizer != GNNTRAIN_SGD && d->optimizer != GNNTRAIN_ADAM && d->optimizer != GNNTRAIN_ADAMW) { err = "unknown optimizer"; return false; }
+  if (d->state_8bit && d->optimizer != GNNTRAIN_ADAMW) { err = "state_8bit needs GNNTRAIN_ADAMW"; return false; }
   if (d->alpha_hist < 1) { err = "alpha_hist must be at least 1"; return false; }
   const gnnstage_t *last = d->stages[d->n_stages - 1];
   x.n = gnnstage_query(last, GNNSTAGE_Q_VERTICES, 0);
@@ -250,9 +252,11 @@ Layout make_layout(const gnntrain_desc *d, const Dims &x) {
     off = align256(off + bytes);
     return at;
   };
-  const size_t moments = d->optimizer == GNNTRAIN_ADAM ? sizeof(float) * (size_t)x.n_param_elems : 0;
+  const size_t moments = d->optimizer == GNNTRAIN_SGD ? 0 : (d->state_8bit ? 1 : sizeof(float)) * (size_t)x.n_param_elems;
   l.m = take(moments);
   l.v = take(moments);
+  l.m_scale = take(d->state_8bit ? moments / 32 : 0);
+  l.v_scale = take(d->state_8bit ? moments / 32 : 0);
   if (!x.fused) {
     l.logits = take(sizeof(float) * (size_t)x.head_rows * x.Cp);
     l.dlogits = take((size_t)x.elt * x.n * x.Cp);
@@ -288,7 +292,8 @@ struct gnntrain {
   const int32_t *labels = nullptr;
   const uint8_t *mask = nullptr;
   int64_t n_train = 0;
-  int optimizer = 0, shuffle = 0, alpha_hist = 1, history_swap = 0;
+  int optimizer = 0, state_bits = 32, shuffle = 0, alpha_hist = 1, history_swap = 0;
+  std::vector<gnntrain_adamw_tensor> adamw;  // GNNTRAIN_ADAMW: the parameters as its step takes them
   float lr = 0, beta1 = 0, beta2 = 0, eps = 0, wd = 0;
   uint64_t seed = 0;
   int64_t step = 0;
@@ -542,9 +547,34 @@ extern "C" int gnntrain_create(const gnntrain_desc *d, gnntrain_t **out) try {
   tr->seed = d->seed;
   tr->ws = static_cast<char *>(d->workspace);
   tr->order.assign((size_t)x.K, 0);
-  if (tr->optimizer == GNNTRAIN_ADAM && x.n_param_elems > 0) {
-    const size_t bytes = sizeof(float) * (size_t)x.n_param_elems;
+  if (tr->optimizer == GNNTRAIN_ADAMW) {
+    tr->state_bits = d->state_8bit ? 8 : 32;
+    const size_t state = d->state_8bit ? 1 : sizeof(float);
+    for (size_t i = 0; i < tr->params.size(); ++i) {
+      const gnntrain_param &p = tr->params[i];
+      const size_t at = tr->moment_off[i];
+      gnntrain_adamw_tensor t{};
+      t.p = p.master;
+      t.g = p.grad;
+      t.g_dtype = GNNSTAGE_F32;
+      t.compute = p.compute;
+      t.compute_dtype = p.compute_dtype;
+      t.m = tr->at<char>(lay.m) + state * at;
+      t.v = tr->at<char>(lay.v) + state * at;
+      t.m_scale = d->state_8bit ? tr->at<uint8_t>(lay.m_scale) + at / 32 : nullptr;
+      t.v_scale = d->state_8bit ? tr->at<uint8_t>(lay.v_scale) + at / 32 : nullptr;
+      t.count = p.count;
+      t.weight_decay = d->weight_decay;
+      tr->adamw.push_back(t);
+    }
+    err = adamw_check(tr->adamw.data(), (int)tr->adamw.size(), tr->state_bits);
+    if (err.empty() && !(d->beta1 >= 0.f && d->beta1 < 1.f && d->beta2 >= 0.f && d->beta2 < 1.f)) err = "beta1 and beta2 must be in [0, 1)";
+    if (!err.empty()) return bad(GNNSTAGE_EINVAL, "AdamW: " + err);
+  }
+  if (tr->optimizer != GNNTRAIN_SGD && x.n_param_elems > 0) {
+    const size_t bytes = (d->state_8bit ? 1 : sizeof(float)) * (size_t)x.n_param_elems, scales = d->state_8bit ? bytes / 32 : 0;
     if (launch_fill_zero(tr->at<char>(lay.m), bytes, nullptr) != 0 || launch_fill_zero(tr->at<char>(lay.v), bytes, nullptr) != 0 ||
+        (scales > 0 && (launch_fill_zero(tr->at<char>(lay.m_scale), scales, nullptr) != 0 || launch_fill_zero(tr->at<char>(lay.v_scale), scales, nullptr) != 0)) ||
         hipDeviceSynchronize() != hipSuccess)
       return bad(GNNSTAGE_EHIP, "clearing the optimiser state failed");
   }
@@ -677,9 +707,12 @@ extern "C" int gnntrain_epoch(gnntrain_t *tr, int64_t epoch, float *loss, void *
   TRAIN_HIP(tr, launch_sum(row_loss, x.n, inv_n, tr->at<float>(lay.scratch), tr->at<float>(lay.loss), stream));
   // ---- weight update
   ++tr->step;
-  const bool adam = tr->optimizer == GNNTRAIN_ADAM;
+  const bool adam = tr->optimizer == GNNTRAIN_ADAM, adamw = tr->optimizer == GNNTRAIN_ADAMW;
+  if (adamw)
+    TRAIN_HIP(tr, launch_adamw(tr->adamw.data(), (int)tr->adamw.size(), tr->state_bits, AdamwRates{tr->lr, tr->beta1, tr->beta2, tr->eps}, nullptr, tr->step,
+                               tr->seed, stream));
   std::vector<Update> updates;
-  for (size_t i = 0; i < tr->params.size(); ++i) {
+  for (size_t i = 0; !adamw && i < tr->params.size(); ++i) {
     const gnntrain_param &p = tr->params[i];
     Update u{p.master, p.grad, adam ? tr->at<float>(lay.m) + tr->moment_off[i] : nullptr, adam ? tr->at<float>(lay.v) + tr->moment_off[i] : nullptr,
              p.compute, p.compute_dtype, p.count};
