@@ -141,6 +141,35 @@ int gnntrain_head_xent(const void *h, int64_t ld_h, const void *W, int32_t dtype
                        const uint8_t *mask, int64_t rows, int32_t d, int32_t n_classes, float inv_n_train, float *row_loss, void *dh,
                        int64_t ld_dh, float *dW, float *db, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* What logits answer, per row, with z = logits + bias:
+ *   logp     log softmax(z) at the row's class ids[r] (0 where that is outside [0, n_classes)); needs ids
+ *   entropy  -sum_c p_c log p_c, p = softmax(z), in nats
+ *   norm     (largest z that is a number, log sum_c exp(z_c - largest z)): what gnntrain_logprobs_grad takes, rows x 2
+ *   top_ids, top_logp  the n_top classes of the largest z in their order, of equals the lower class first, and their log softmax, rows x n_top
+ * Each output but the last two, which n_top > 0 asks for, may be NULL.  Sums are fp32; a row that is sure of its given class has a log probability with all its digits.
+ * A logit of minus infinity is a class left out: probability 0, last in the order.  A row whose every logit is minus infinity, or with infinity or a NaN among
+ * them, has NaN for every number but norm's first; a NaN is in no order, and ids that are not there are -1.  A row whose mask byte is 0 (mask NULL: none) takes
+ * no part: it is not read, and gets zeros, classes -1 and their log probabilities minus infinity.
+ * logits: DEVICE rows x n_classes of dtype, leading dimension ld >= n_classes, aligned to its elements; bias: DEVICE fp32 n_classes or NULL; ids, mask: DEVICE, by row, or NULL.
+ * n_classes in [1, 2^24], n_top in [0, 64] and n_classes at most.  workspace: DEVICE, 256-byte aligned, of gnntrain_logprobs_workspace_size(), nothing in it
+ * has to be cleared or kept; calls that overlap in time need workspaces of their own, and so do graphs that are replayed side by side.  Outputs may not
+ * overlap inputs.  The call only launches kernels (asynchronous, may be captured); the same call gives the same bits.  Message of an error: gnntrain_last_error(NULL). */
+size_t gnntrain_logprobs_workspace_size(int64_t rows, int32_t n_classes, int32_t n_top);
+int gnntrain_logprobs(const void *logits, int32_t dtype, int64_t ld, const float *bias, const int32_t *ids, const uint8_t *mask, int64_t rows, int32_t n_classes,
+                      int32_t n_top, float *logp, float *entropy, float *norm, int32_t *top_ids, float *top_logp, void *workspace, size_t workspace_bytes,
+                      void *hip_stream);
+
+/* Gradient of the logits from those of logp and entropy (g_logp, g_entropy: DEVICE fp32 by row; NULL: zeros):
+ *   dlogits_c = g_logp ([c = id] - p_c) - g_entropy p_c (log p_c + entropy);  dbias_c += sum over the rows of dlogits_c before it is rounded
+ * logits, bias, ids, mask as in the forward call, logp (with g_logp), entropy (with g_entropy) and norm what it gave.  A row without a class in [0, n_classes) has
+ * no part in g_logp; a row whose mask byte is 0 gets zeros and is not read.  dlogits: DEVICE rows x n_classes of dl_dtype, leading dimension ld_dl >= n_classes (columns
+ * behind n_classes stay as they are); it may be logits, with the same type and leading dimension.  dbias: DEVICE fp32 n_classes or NULL.  Sums in a fixed order.
+ * workspace as above, of gnntrain_logprobs_grad_workspace_size(). */
+size_t gnntrain_logprobs_grad_workspace_size(int64_t rows, int32_t n_classes);
+int gnntrain_logprobs_grad(const void *logits, int32_t dtype, int64_t ld, const float *bias, const int32_t *ids, const uint8_t *mask, int64_t rows, int32_t n_classes,
+                           const float *logp, const float *entropy, const float *norm, const float *g_logp, const float *g_entropy, void *dlogits, int32_t dl_dtype,
+                           int64_t ld_dl, float *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* out[0] = scale * sum of x[0 .. n), added in a fixed order (reproducible).  scratch: DEVICE, 1024 floats. */
 int gnntrain_sum(const float *x, int64_t n, float scale, float *scratch, float *out, void *hip_stream);
 

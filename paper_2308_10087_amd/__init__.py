@@ -10,6 +10,7 @@ from .binding import (  # noqa: F401
     GNNTRAIN_ADAM, GNNTRAIN_SGD, GnnTrainer, gnntrain_adam_step, gnntrain_chunk_order, gnntrain_sgd_step,
     gnntrain_softmax_xent, gnntrain_sum, gnntrain_sum_static, gnnstage_partition_chunks, gnnstage_permute_csr,
     gnnstage_debug_gather_rate, gnntrain_head_xent, gnntrain_head_xent_workspace_size, gnnstage_rows8_load, gnnstage_rows8_store,
-    GNNTRAIN_ADAMW, gnntrain_adamw_step, gnntrain_adamw_tensors,
+    GNNTRAIN_ADAMW, gnntrain_adamw_step, gnntrain_adamw_tensors, gnntrain_logprobs, gnntrain_logprobs_grad,
+    gnntrain_logprobs_grad_workspace_size, gnntrain_logprobs_workspace_size,
     gnnstage_rows8_weight_grad, gnnstage_rows8_weight_grad_workspace_size,
 )

@@ -180,6 +180,16 @@ def _load():
     lib.gnntrain_sgd_step.restype = C.c_int
     lib.gnntrain_sgd_step.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_float,
                                       C.c_void_p]
+    lib.gnntrain_logprobs_workspace_size.restype = C.c_size_t
+    lib.gnntrain_logprobs_workspace_size.argtypes = [C.c_int64, C.c_int32, C.c_int32]
+    lib.gnntrain_logprobs.restype = C.c_int
+    lib.gnntrain_logprobs.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.gnntrain_logprobs_grad_workspace_size.restype = C.c_size_t
+    lib.gnntrain_logprobs_grad_workspace_size.argtypes = [C.c_int64, C.c_int32]
+    lib.gnntrain_logprobs_grad.restype = C.c_int
+    lib.gnntrain_logprobs_grad.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p,
+                                           C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     lib.gnntrain_adamw_step.restype = C.c_int
     lib.gnntrain_adamw_step.argtypes = [C.POINTER(gnntrain_adamw_tensor), C.c_int32, C.c_int32, C.c_float, C.c_float, C.c_float, C.c_float, C.c_void_p,
                                         C.c_int64, C.c_uint64, C.c_void_p]
@@ -747,6 +757,81 @@ def gnntrain_head_xent(h, W, bias, labels, mask, inv_n_train: float, row_loss, w
     ptr = lambda t: None if t is None else t.data_ptr()
     rc = _launch(name, dev, lib.gnntrain_head_xent, h.data_ptr(), ld_h, W.data_ptr(), dt, ptr(bias), labels.data_ptr(), ptr(mask), rows, d,
                  n_classes, float(inv_n_train), row_loss.data_ptr(), ptr(dh), ld_dh, ptr(dW), ptr(db), ws, size)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnntrain_last_error(None).decode())
+
+
+def gnntrain_logprobs_workspace_size(rows: int, n_classes: int, n_top: int = 0) -> int:
+    size = int(lib.gnntrain_logprobs_workspace_size(int(rows), int(n_classes), int(n_top)))
+    if size == 0:
+        raise GnnStageError(-1, lib.gnntrain_last_error(None).decode())
+    return size
+
+
+def _row_inputs(name: str, logits, bias, ids, mask):
+    import torch
+    dt, dev = _dtype_code(name, "logits", logits), logits.device
+    ld = _matrix(name, "logits", logits, None, logits.dtype, dev)
+    rows, n_classes = logits.shape
+    for what, t, shape, dtype in (("bias", bias, (n_classes,), torch.float32), ("ids", ids, (rows,), torch.int32), ("mask", mask, (rows,), torch.uint8)):
+        if t is not None:
+            _tensor(name, what, t, shape, dtype, dev)
+    return dt, ld
+
+
+def gnntrain_logprobs(logits, bias, ids, mask, logp, entropy, norm, workspace, top_ids=None, top_logp=None) -> None:
+    """Per row of ``logits`` (fp32 or bf16 [rows, n_classes], + ``bias`` fp32 or None): ``logp`` fp32 [rows], the log probability of the class ``ids`` (int32 [rows]);
+    ``entropy`` fp32 [rows]; ``norm`` fp32 [rows, 2], for gnntrain_logprobs_grad; ``top_ids`` int32 and ``top_logp`` fp32 [rows, n], the n best classes.  Each but the
+    logits may be None; mask uint8 [rows]."""
+    import torch
+    name = "gnntrain_logprobs"
+    dt, ld = _row_inputs(name, logits, bias, ids, mask)
+    rows, n_classes = logits.shape
+    n_top = 0
+    if (top_ids is None) != (top_logp is None):
+        _refuse(name, "top_ids and top_logp go together")
+    if top_ids is not None:
+        if top_ids.dim() != 2:
+            _refuse(name, "top_ids must be a matrix")
+        n_top = top_ids.shape[1]
+    for what, t, shape, dtype in (("logp", logp, (rows,), torch.float32), ("entropy", entropy, (rows,), torch.float32), ("norm", norm, (rows, 2), torch.float32),
+                                  ("top_ids", top_ids, (rows, n_top), torch.int32), ("top_logp", top_logp, (rows, n_top), torch.float32)):
+        if t is not None:
+            _tensor(name, what, t, shape, dtype, logits.device)
+    ws, size = _room(name, workspace, logits.device)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    rc = _launch(name, logits.device, lib.gnntrain_logprobs, logits.data_ptr(), dt, ld, ptr(bias), ptr(ids), ptr(mask), rows, n_classes, n_top, ptr(logp),
+                 ptr(entropy), ptr(norm), ptr(top_ids), ptr(top_logp), ws, size)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnntrain_last_error(None).decode())
+
+
+def gnntrain_logprobs_grad_workspace_size(rows: int, n_classes: int) -> int:
+    size = int(lib.gnntrain_logprobs_grad_workspace_size(int(rows), int(n_classes)))
+    if size == 0:
+        raise GnnStageError(-1, lib.gnntrain_last_error(None).decode())
+    return size
+
+
+def gnntrain_logprobs_grad(logits, bias, ids, mask, logp, entropy, norm, g_logp, g_entropy, dlogits, workspace, dbias=None) -> None:
+    """``dlogits`` (fp32 or bf16 [rows, n_classes], or ``logits`` itself) from the gradients ``g_logp``, ``g_entropy`` (fp32 [rows], or None) of what gnntrain_logprobs
+    gave; ``dbias`` (fp32 [n_classes]) is added to."""
+    import torch
+    name = "gnntrain_logprobs_grad"
+    dt, ld = _row_inputs(name, logits, bias, ids, mask)
+    rows, n_classes = logits.shape
+    dl_dt = _dtype_code(name, "dlogits", dlogits)
+    ld_dl = _matrix(name, "dlogits", dlogits, (rows, n_classes), dlogits.dtype, logits.device)
+    if rows == 1 and dlogits.data_ptr() == logits.data_ptr():
+        ld_dl = ld  # (a single row's leading dimension means nothing)
+    for what, t, shape in (("logp", logp, (rows,)), ("entropy", entropy, (rows,)), ("norm", norm, (rows, 2)), ("g_logp", g_logp, (rows,)),
+                           ("g_entropy", g_entropy, (rows,)), ("dbias", dbias, (n_classes,))):
+        if t is not None:
+            _tensor(name, what, t, shape, torch.float32, logits.device)
+    ws, size = _room(name, workspace, logits.device)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    rc = _launch(name, logits.device, lib.gnntrain_logprobs_grad, logits.data_ptr(), dt, ld, ptr(bias), ptr(ids), ptr(mask), rows, n_classes, ptr(logp),
+                 ptr(entropy), ptr(norm), ptr(g_logp), ptr(g_entropy), dlogits.data_ptr(), dl_dt, ld_dl, ptr(dbias), ws, size)
     if rc != 0:
         raise GnnStageError(rc, lib.gnntrain_last_error(None).decode())
 
