@@ -398,6 +398,31 @@ int gnnstage_rows8_weight_grad(const int8_t *q, int64_t ld_q, const uint8_t *sca
                                size_t workspace_bytes, void *hip_stream);
 
 /*
+ * Rows kept in 4 bits (OCP's MXFP4) and their product: a classifier's weights (or rows of a level) to answer from.  Blocks of 32 columns share a
+ * factor 2^e, e the least whole number with max |x| <= 7 * 2^e, held within [-120, 125]; a value is the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times it, of two as near
+ * the one with an even code, with its sign.  Codes 0 .. 7 stand for these, 8 more for minus; a byte of q holds two columns, the first one in its low half.
+ * scale holds the byte e + 127; 255: the block had an infinity or a NaN, all of it is NaN.
+ * q: DEVICE, 16-byte aligned, rows x ld_q bytes, ld_q a multiple of 16 and at least 16 per 32 columns (zeros from d on, to whole blocks); scale: DEVICE, rows x ld_s,
+ * ld_s >= (d + 31) / 32.  x, out: DEVICE, of dtype (GNNSTAGE_F32 / GNNSTAGE_BF16), leading dimensions of any size from the width on, aligned to their elements.
+ * d in [1, 65536].
+ *   gnnstage_rows4_store          q, scale from x (rows x d)
+ *   gnnstage_rows4_store_columns  the same from the columns of x (d x rows, ld_x >= rows): a classifier's W (d x n_classes) as one row per class
+ *   gnnstage_rows4_load           x from q, scale
+ *   gnnstage_rows4_product        out (rows x others) = stored rows times other stored rows, over their d columns, + bias (DEVICE fp32, others elements, or NULL): products
+ *                                 of exactly the stored values, fp32 sums in a fixed order, rounded once.  others at most 2^29
+ * They only launch kernels on hip_stream.  Message of an error: gnnstage_last_error(NULL).
+ */
+int gnnstage_rows4_store(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t d, uint8_t *q, int64_t ld_q, uint8_t *scale,
+                         int64_t ld_s, void *hip_stream);
+int gnnstage_rows4_store_columns(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t d, uint8_t *q, int64_t ld_q, uint8_t *scale,
+                                 int64_t ld_s, void *hip_stream);
+int gnnstage_rows4_load(const uint8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, int64_t rows, int32_t d, void *x, int32_t dtype,
+                        int64_t ld_x, void *hip_stream);
+int gnnstage_rows4_product(const uint8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, int64_t rows, const uint8_t *other_q, int64_t ld_oq,
+                           const uint8_t *other_scale, int64_t ld_os, int64_t others, int32_t d, const float *bias, void *out, int32_t dtype,
+                           int64_t ld_out, void *hip_stream);
+
+/*
  * Diagnostic: what this GPU's memory system gives the access pattern of the aggregation (Algorithm 1's AGGREGATE
  * line reads one embedding row per neighbour), with no arithmetic and no index traffic around it.  Every 16-lane
  * group reads whole rows of row_bytes (a multiple of 256, at most 4096) at pseudo-random row numbers, eight rows in

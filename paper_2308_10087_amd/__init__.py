@@ -12,5 +12,6 @@ from .binding import (  # noqa: F401
     gnnstage_debug_gather_rate, gnntrain_head_xent, gnntrain_head_xent_workspace_size, gnnstage_rows8_load, gnnstage_rows8_store,
     GNNTRAIN_ADAMW, gnntrain_adamw_step, gnntrain_adamw_tensors, gnntrain_logprobs, gnntrain_logprobs_grad,
     gnntrain_logprobs_grad_workspace_size, gnntrain_logprobs_workspace_size,
+    gnnstage_rows4_load, gnnstage_rows4_product, gnnstage_rows4_store, gnnstage_rows4_store_columns,
     gnnstage_rows8_weight_grad, gnnstage_rows8_weight_grad_workspace_size,
 )

@@ -190,6 +190,14 @@ def _load():
     lib.gnntrain_logprobs_grad.restype = C.c_int
     lib.gnntrain_logprobs_grad.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p,
                                            C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    for name in ("gnnstage_rows4_store", "gnnstage_rows4_store_columns"):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+    lib.gnnstage_rows4_load.restype = C.c_int
+    lib.gnnstage_rows4_load.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]
+    lib.gnnstage_rows4_product.restype = C.c_int
+    lib.gnnstage_rows4_product.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int32,
+                                           C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]
     lib.gnntrain_adamw_step.restype = C.c_int
     lib.gnntrain_adamw_step.argtypes = [C.POINTER(gnntrain_adamw_tensor), C.c_int32, C.c_int32, C.c_float, C.c_float, C.c_float, C.c_float, C.c_void_p,
                                         C.c_int64, C.c_uint64, C.c_void_p]
@@ -502,6 +510,68 @@ def gnnstage_rows8_weight_grad(q, scale, dY, dW, workspace, dbias=None) -> None:
     ws, size = _room(name, workspace, dev)
     rc = _launch(name, dev, lib.gnnstage_rows8_weight_grad, q.data_ptr(), ld_q, scale.data_ptr(), ld_s, dY.data_ptr(), dt, ld_dy, q.shape[0], d,
                  d_out, dW.data_ptr(), None if dbias is None else dbias.data_ptr(), ws, size)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
+
+
+def _stored4(name: str, q, scale, rows, d, device):
+    import torch
+    blocks = (d + 31) // 32
+    ld_q = _matrix(name, "q", q, (rows, 16 * blocks), torch.uint8, device)
+    ld_s = _matrix(name, "scale", scale, (rows, blocks), torch.uint8, device)
+    return (ld_q + 15) // 16 * 16 if rows <= 1 else ld_q, ld_s
+
+
+def gnnstage_rows4_store(x, q, scale) -> None:
+    """Keeps the rows of ``x`` (fp32 or bf16, rows x d) in 4 bits: ``q`` uint8 [rows, 16 per 32 columns], ``scale`` uint8 [rows, one per 32 columns]."""
+    name = "gnnstage_rows4_store"
+    dt = _dtype_code(name, "x", x)
+    ld_x = _matrix(name, "x", x, None, x.dtype, x.device)
+    rows, d = x.shape
+    ld_q, ld_s = _stored4(name, q, scale, rows, d, x.device)
+    rc = _launch(name, x.device, lib.gnnstage_rows4_store, x.data_ptr(), dt, ld_x, rows, d, q.data_ptr(), ld_q, scale.data_ptr(), ld_s)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
+
+
+def gnnstage_rows4_store_columns(x, q, scale) -> None:
+    """Keeps the columns of ``x`` (fp32 or bf16, d x rows: a classifier's weights) in 4 bits, one row of ``q`` and ``scale`` each."""
+    name = "gnnstage_rows4_store_columns"
+    dt = _dtype_code(name, "x", x)
+    ld_x = _matrix(name, "x", x, None, x.dtype, x.device)
+    d, rows = x.shape
+    ld_q, ld_s = _stored4(name, q, scale, rows, d, x.device)
+    rc = _launch(name, x.device, lib.gnnstage_rows4_store_columns, x.data_ptr(), dt, ld_x, rows, d, q.data_ptr(), ld_q, scale.data_ptr(), ld_s)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
+
+
+def gnnstage_rows4_load(q, scale, x) -> None:
+    """Restores rows into ``x`` (fp32 or bf16, rows x d)."""
+    name = "gnnstage_rows4_load"
+    dt = _dtype_code(name, "x", x)
+    ld_x = _matrix(name, "x", x, None, x.dtype, x.device)
+    rows, d = x.shape
+    ld_q, ld_s = _stored4(name, q, scale, rows, d, x.device)
+    rc = _launch(name, x.device, lib.gnnstage_rows4_load, q.data_ptr(), ld_q, scale.data_ptr(), ld_s, rows, d, x.data_ptr(), dt, ld_x)
+    if rc != 0:
+        raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
+
+
+def gnnstage_rows4_product(q, scale, other_q, other_scale, d: int, out, bias=None) -> None:
+    """``out`` (fp32 or bf16 [rows, others]) = stored rows times other stored rows over their ``d`` columns, + ``bias`` fp32 [others]."""
+    import torch
+    name = "gnnstage_rows4_product"
+    dt = _dtype_code(name, "out", out)
+    dev = out.device
+    ld_out = _matrix(name, "out", out, None, out.dtype, dev)
+    rows, others = out.shape
+    ld_q, ld_s = _stored4(name, q, scale, rows, int(d), dev)
+    ld_oq, ld_os = _stored4(name, other_q, other_scale, others, int(d), dev)
+    if bias is not None:
+        _tensor(name, "bias", bias, (others,), torch.float32, dev)
+    rc = _launch(name, dev, lib.gnnstage_rows4_product, q.data_ptr(), ld_q, scale.data_ptr(), ld_s, rows, other_q.data_ptr(), ld_oq, other_scale.data_ptr(), ld_os,
+                 others, int(d), None if bias is None else bias.data_ptr(), out.data_ptr(), dt, ld_out)
     if rc != 0:
         raise GnnStageError(rc, lib.gnnstage_last_error(None).decode())
 

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgnnstage.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-SOURCES = ["gnnstage.hip", "spmm.hip", "dense.hip", "gemm.hip", "misc.hip", "ln.hip", "train.hip", "adamw.hip", "logprobs.hip", "head.hip", "head32.hip", "rows8.hip", "plan.cpp", "partition.cpp"]
+SOURCES = ["gnnstage.hip", "spmm.hip", "dense.hip", "gemm.hip", "misc.hip", "ln.hip", "train.hip", "adamw.hip", "logprobs.hip", "head.hip", "head32.hip", "rows8.hip", "rows4.hip", "plan.cpp", "partition.cpp"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # packed-fp32 VALU forms are switched off on purpose: hipcc -O3 would form them by itself from ordinary
          # float code, and some of those forms have given wrong results on this hardware

@@ -1,0 +1,421 @@
+// Rows kept in 4 bits (OCP's MXFP4) and their product: blocks of 32 columns of a row share a power of two.
+//
+//   a = max |x| over the block, e = the least whole number with a <= 7 * 2^e, held within [-120, 125]
+//   q = the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 to |x| / 2^e (of two as near the one whose code is even), with x's sign;  the value is then q * 2^e
+//
+// A value is off by at most half the distance of its neighbours, 2^e in the largest binade.  (7 instead of 6 as the border: what lies between is as
+// near to 6 as a value can be to 5, and a whole block keeps one more bit.)  The factor is kept as the byte e + 127; 255 is a block with an
+// infinity or a NaN among its values, all of which is NaN.
+//
+// Products are those of exactly the stored values: two codes multiply to at most 7 bits, the matrix cores add them up in fp32 with their blocks' factors.
+#include <hip/hip_runtime.h>
+#include "guard.h"
+
+#include <algorithm>
+#include <string>
+
+#include "../../include/gnnstage.h"
+#include "common.h"
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// rows start anywhere: the memory system takes vectors at any address of their elements
+typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
+typedef bf16_t bf16x8_u __attribute__((ext_vector_type(8), aligned(2)));
+typedef bf16_t bf16x4_u __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32_u __attribute__((aligned(1)));
+
+// columns c .. c + 7 of a row; zeros from d on
+template <typename T>
+__device__ inline void load8(const T *row, int c, int d, float (&v)[8]) {
+  if (c + 8 <= d) {
+    if constexpr (sizeof(T) == 2) {
+      const bf16x8_u x = *reinterpret_cast<const bf16x8_u *>(row + c);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) v[t] = (float)x[t];
+    } else {
+      const f32x4_u x = *reinterpret_cast<const f32x4_u *>(row + c), y = *reinterpret_cast<const f32x4_u *>(row + c + 4);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        v[t] = x[t];
+        v[4 + t] = y[t];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = c + t < d ? (float)row[c + t] : 0.f;
+  }
+}
+
+// The factor of a block whose largest magnitude has the bits a: its byte, and 2^-e (0: not finite).
+__device__ __forceinline__ uint32_t factor_of(uint32_t a, float &inv) {
+  if (a >= 0x7f800000u) {
+    inv = 0.f;
+    return 255;
+  }
+  // a = f 2^(E - 127) <= 7 2^e = 1.75 2^(2 + e): e = E - 129 up to f = 1.75, one more beyond
+  const int e = min(max((int)(a >> 23) - 129 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0), -120), 125);
+  inv = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
+  return (uint32_t)(e + 127);
+}
+// The code of x / 2^e.  In the binades [0, 2), [2, 4), [4, 8) numbers are 1/2, 1, 2 apart: added to 1.5 2^23 times that the value is rounded to one of them,
+// to the even of two as near, which is the even code.
+__device__ __forceinline__ uint32_t code_of(float x, float inv) {
+  const float y = fabsf(x) * inv;
+  const float grid = y < 2.f ? 6291456.f : y < 4.f ? 12582912.f : 25165824.f;
+  const uint32_t from = y < 2.f ? 0u : y < 4.f ? 2u : 4u;
+  const uint32_t n = __builtin_bit_cast(uint32_t, y + grid) & 0xfu;
+  return min(n + from, 7u) | ((__builtin_bit_cast(uint32_t, x) >> 28) & 8u);
+}
+
+// A thread per eight columns, four neighbouring lanes per block (quads never straddle rows: a row has whole blocks).
+template <typename T>
+__global__ __launch_bounds__(256) void rows4_store_kernel(const T *x, int64_t ld, int64_t rows, int d, int blocks, uint8_t *q, int64_t ld_q, uint8_t *scale,
+                                                          int64_t ld_s) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int per_row = blocks * 4;
+  const int64_t r = i / per_row;
+  if (r >= rows) return;
+  const int g = (int)(i - r * per_row), c = g * 8;
+  float v[8];
+  load8<T>(x + (size_t)(r * ld), c, d, v);
+  uint32_t a = 0;  // the largest magnitude, compared as bits: infinities and NaNs are above every number
+#pragma unroll
+  for (int t = 0; t < 8; ++t) a = max(a, __builtin_bit_cast(uint32_t, v[t]) & 0x7fffffffu);
+  a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xf, 0xf, true));  // lanes 1 0 3 2 of the quad
+  a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x4E, 0xf, 0xf, true));  // lanes 2 3 0 1
+  float inv;
+  const uint32_t byte = factor_of(a, inv);
+  uint32_t w = 0;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) w |= (byte == 255 ? 0u : code_of(v[t], inv)) << (4 * t);
+  *reinterpret_cast<uint32_t *>(q + (size_t)(r * ld_q) + g * 4) = w;
+  if ((g & 3) == 0) scale[(size_t)(r * ld_s) + (g >> 2)] = (uint8_t)byte;
+}
+
+// The columns of x (d x rows) as rows: a thread per block, 64 columns and four blocks down a workgroup.
+template <typename T>
+__global__ __launch_bounds__(256) void rows4_store_columns_kernel(const T *x, int64_t ld, int64_t rows, int d, int blocks, uint8_t *q, int64_t ld_q, uint8_t *scale,
+                                                                  int64_t ld_s) {
+  const int64_t r = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  const int block = (int)blockIdx.y * 4 + (threadIdx.x >> 6);
+  if (r >= rows || block >= blocks) return;
+  float v[32];
+  uint32_t a = 0;
+#pragma unroll
+  for (int t = 0; t < 32; ++t) {
+    const int k = block * 32 + t;
+    v[t] = k < d ? (float)x[(size_t)(k * ld) + r] : 0.f;
+    a = max(a, __builtin_bit_cast(uint32_t, v[t]) & 0x7fffffffu);
+  }
+  float inv;
+  const uint32_t byte = factor_of(a, inv);
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int t = 0; t < 32; ++t) w[t >> 3] |= (byte == 255 ? 0u : code_of(v[t], inv)) << (4 * (t & 7));
+  *reinterpret_cast<u32x4 *>(q + (size_t)(r * ld_q) + block * 16) = u32x4{w[0], w[1], w[2], w[3]};
+  scale[(size_t)(r * ld_s) + block] = (uint8_t)byte;
+}
+
+// A thread per eight columns
+template <typename T>
+__global__ __launch_bounds__(256) void rows4_load_kernel(const uint8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, int64_t rows, int d, int per_row, T *x,
+                                                         int64_t ld) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t r = i / per_row;
+  if (r >= rows) return;
+  const int g = (int)(i - r * per_row), c = g * 8;
+  const uint32_t w = *reinterpret_cast<const uint32_t *>(q + (size_t)(r * ld_q) + g * 4);
+  const uint32_t byte = scale[(size_t)(r * ld_s) + (g >> 2)];
+  const float f = byte == 255 ? NAN : __builtin_bit_cast(float, byte << 23);
+  float v[8];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    const uint32_t code = w >> (4 * t), n = code & 7u;
+    // 1 + bit/2 in binade 2^(n / 2 - 1); the two below are 0 and 1/2
+    const float size = n < 2u ? 0.5f * (float)n : __builtin_bit_cast(float, ((n >> 1) + 126u) << 23 | (n & 1u) << 22);
+    v[t] = (code & 8u ? -size : size) * f;
+  }
+  T *row = x + (size_t)(r * ld) + c;
+  if (c + 8 <= d) {
+    if constexpr (sizeof(T) == 2) {
+      bf16x8_u o;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[t] = (bf16_t)v[t];
+      *reinterpret_cast<bf16x8_u *>(row) = o;
+    } else {
+      f32x4_u lo, hi;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        lo[t] = v[t];
+        hi[t] = v[4 + t];
+      }
+      *reinterpret_cast<f32x4_u *>(row) = lo;
+      *reinterpret_cast<f32x4_u *>(row + 4) = hi;
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+      if (c + t < d) row[t] = (T)v[t];
+  }
+}
+
+// ---- the product ----------------------------------------------------------------------------------------------------
+struct ProductArgs {
+  const uint8_t *a, *a_scale, *b, *b_scale;
+  int64_t ld_a, ld_as, ld_b, ld_bs;
+  int64_t M, N;
+  int32_t blocks;     // of 32 columns
+  const float *bias;  // by column of the result, or NULL
+  void *out;
+  int64_t ld_out;
+  int64_t row_tiles, tiles;
+  uint32_t per_xcd;
+};
+// Operands of a row: 256 columns at a time, eight blocks.  Matrix instructions take 64 columns, 32 from each half of the wave; here the lower half has the blocks
+// 0 .. 3, the upper one 4 .. 7, one per instruction: a lane's are 64 bytes side by side, and their factors one word, a byte for each instruction.
+struct Operand {
+  u32x4 q[4];
+  uint32_t scale;
+  __device__ __forceinline__ void load(const uint8_t *row, const uint8_t *scales, int block, int blocks) {
+    const int left = blocks - block;
+    if (left >= 4) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) q[s] = *reinterpret_cast<const u32x4 *>(row + (size_t)(block + s) * 16);
+      scale = *reinterpret_cast<const u32_u *>(scales + block);
+    } else {
+      scale = 0x7f7f7f7fu;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        q[s] = u32x4{0, 0, 0, 0};
+        if (s < left) {
+          q[s] = *reinterpret_cast<const u32x4 *>(row + (size_t)(block + s) * 16);
+          scale = (scale & ~(0xffu << (8 * s))) | (uint32_t)scales[block + s] << (8 * s);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ i32x8 operator()(int s) const { return i32x8{(int)q[s][0], (int)q[s][1], (int)q[s][2], (int)q[s][3], 0, 0, 0, 0}; }
+};
+template <int S>
+__device__ __forceinline__ f32x16 multiply(const Operand &a, const Operand &b, f32x16 c) {
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a(S), b(S), c, 4, 4, S, (int)a.scale, S, (int)b.scale);  // 4: e2m1
+}
+
+constexpr int kAcross = 4;  // columns of the result a lane: 128 a wave
+
+// A wave per tile of 32 DOWN rows and 128 columns.  A lane's columns are side by side (column 4 l + t is the t-th instruction's l-th), so that rows are
+// written 256 (512) bytes at a time from the registers.  Register i of lane l: row 8 (i / 4) + 4 (l / 32) + i % 4.
+template <typename O, int DOWN>
+__global__ __launch_bounds__(256) void rows4_product_kernel(const ProductArgs p) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, h = lane >> 5;
+  // an XCD has tiles that follow one another: the columns' operands are read once into one L2
+  const int64_t tile = ((int64_t)(blockIdx.x & 7) * p.per_xcd + (blockIdx.x >> 3)) * 4 + wave;
+  if (blockIdx.x >> 3 >= p.per_xcd || tile >= p.tiles) return;
+  const int64_t n0 = tile / p.row_tiles * (32 * kAcross), m0 = tile % p.row_tiles * (32 * DOWN);
+  f32x16 sum[DOWN][kAcross];
+#pragma unroll
+  for (int i = 0; i < DOWN; ++i)
+#pragma unroll
+    for (int t = 0; t < kAcross; ++t)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) sum[i][t][k] = 0.f;
+  for (int block = 0; block < p.blocks; block += 8) {
+    Operand a[DOWN], b[kAcross];
+    // (past the last row or column: that one once more, whatever it gives is not written)
+#pragma unroll
+    for (int i = 0; i < DOWN; ++i) {
+      const int64_t m = min(m0 + 32 * i + l, p.M - 1);
+      a[i].load(p.a + (size_t)(m * p.ld_a), p.a_scale + (size_t)(m * p.ld_as), block + 4 * h, p.blocks);
+    }
+#pragma unroll
+    for (int t = 0; t < kAcross; ++t) {
+      const int64_t n = min(n0 + kAcross * l + t, p.N - 1);
+      b[t].load(p.b + (size_t)(n * p.ld_b), p.b_scale + (size_t)(n * p.ld_bs), block + 4 * h, p.blocks);
+    }
+#pragma unroll
+    for (int i = 0; i < DOWN; ++i)
+#pragma unroll
+      for (int t = 0; t < kAcross; ++t) {
+        sum[i][t] = multiply<0>(a[i], b[t], sum[i][t]);
+        sum[i][t] = multiply<1>(a[i], b[t], sum[i][t]);
+        sum[i][t] = multiply<2>(a[i], b[t], sum[i][t]);
+        sum[i][t] = multiply<3>(a[i], b[t], sum[i][t]);
+      }
+  }
+  const int64_t n = n0 + kAcross * l;
+  const bool whole = n + kAcross <= p.N;
+  float bias[kAcross];
+#pragma unroll
+  for (int t = 0; t < kAcross; ++t) bias[t] = p.bias && n + t < p.N ? p.bias[n + t] : 0.f;
+#pragma unroll
+  for (int i = 0; i < DOWN; ++i)
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int64_t m = m0 + 32 * i + 8 * (k >> 2) + 4 * h + (k & 3);
+      if (m >= p.M) continue;
+      O *out = static_cast<O *>(p.out) + (size_t)(m * p.ld_out) + n;
+      if (whole) {
+        typename std::conditional<sizeof(O) == 2, bf16x4_u, f32x4_u>::type v;
+#pragma unroll
+        for (int t = 0; t < kAcross; ++t) v[t] = (O)(sum[i][t][k] + bias[t]);
+        *reinterpret_cast<decltype(v) *>(out) = v;
+      } else {
+#pragma unroll
+        for (int t = 0; t < kAcross; ++t)
+          if (n + t < p.N) out[t] = (O)(sum[i][t][k] + bias[t]);
+      }
+    }
+}
+
+bool sizes_ok(int64_t rows, int d, std::string &err) {
+  if (rows < 0 || rows > ((int64_t)1 << 40)) { err = "rows must not be negative (nor beyond 2^40)"; return false; }
+  if (d < 1 || d > 65536) { err = "a width must be in [1, 65536]"; return false; }
+  return true;
+}
+bool stored_ok(const void *q, int64_t ld_q, const void *scale, int64_t ld_s, int d, std::string &err) {
+  if (!q || !scale) { err = "q and scale must not be NULL"; return false; }
+  if ((reinterpret_cast<uintptr_t>(q) & 15u) || ld_q % 16 != 0) { err = "q must be 16-byte aligned, its leading dimension a multiple of 16"; return false; }
+  if (ld_q < round_up(d, 32) / 2 || ld_s < (d + 31) / 32) { err = "q rows need 16 bytes per 32 columns, scale rows a byte"; return false; }
+  return true;
+}
+bool matrix_ok(const void *x, int dtype, std::string &err) {
+  if (!x) { err = "a matrix must not be NULL"; return false; }
+  if (reinterpret_cast<uintptr_t>(x) & (dtype == GNNSTAGE_BF16 ? 1u : 3u)) { err = "a matrix is not aligned to its elements"; return false; }
+  return true;
+}
+
+template <typename T>
+int run_store(const T *x, int64_t ld, int64_t rows, int d, bool columns, uint8_t *q, int64_t ld_q, uint8_t *scale, int64_t ld_s, hipStream_t s) {
+  const int blocks = (d + 31) / 32;
+  if (!columns)
+    return for_row_slabs(rows, blocks * 4, [&](int64_t r, int64_t m, unsigned gx) {
+      hipLaunchKernelGGL(rows4_store_kernel<T>, dim3(gx), dim3(256), 0, s, x + (size_t)(r * ld), ld, m, d, blocks, q + (size_t)(r * ld_q), ld_q, scale + (size_t)(r * ld_s), ld_s);
+    });
+  const int gy = (blocks + 3) / 4;
+  const int64_t most = kMostBlocks / gy * 64;
+  for (int64_t r = 0; r < rows; r += most) {
+    const int64_t m = std::min(most, rows - r);
+    hipLaunchKernelGGL(rows4_store_columns_kernel<T>, dim3((unsigned)((m + 63) / 64), (unsigned)gy), dim3(256), 0, s, x + r, ld, m, d, blocks, q + (size_t)(r * ld_q), ld_q,
+                       scale + (size_t)(r * ld_s), ld_s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
+  }
+  return hipSuccess;
+}
+
+template <typename O>
+int run_product(ProductArgs p, hipStream_t s) {
+  const bool few = p.M <= 32;
+  const int down = few ? 32 : 64;
+  const int64_t col_tiles = (p.N + 32 * kAcross - 1) / (32 * kAcross), rows = p.M;
+  // as many rows as a launch takes workgroups for
+  const int64_t most = std::max<int64_t>(1, kMostBlocks / 2 * 4 / col_tiles) * down;
+  const uint8_t *a = p.a, *a_scale = p.a_scale;
+  O *out = static_cast<O *>(p.out);
+  for (int64_t r = 0; r < rows; r += most) {
+    p.M = std::min(most, rows - r);
+    p.a = a + (size_t)(r * p.ld_a);
+    p.a_scale = a_scale + (size_t)(r * p.ld_as);
+    p.out = out + (size_t)(r * p.ld_out);
+    p.row_tiles = (p.M + down - 1) / down;
+    p.tiles = p.row_tiles * col_tiles;
+    const int64_t groups = (p.tiles + 3) / 4;
+    p.per_xcd = (uint32_t)((groups + 7) / 8);
+    hipLaunchKernelGGL((few ? rows4_product_kernel<O, 1> : rows4_product_kernel<O, 2>), dim3(p.per_xcd * 8), dim3(256), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
+  }
+  return hipSuccess;
+}
+
+int store(const char *name, bool columns, const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t d, uint8_t *q, int64_t ld_q, uint8_t *scale, int64_t ld_s,
+          void *hip_stream) {
+  const std::string me = std::string(name) + ": ";
+  std::string err;
+  if (dtype != GNNSTAGE_F32 && dtype != GNNSTAGE_BF16) return stage_error(GNNSTAGE_EINVAL, me + "unknown dtype");
+  if (!sizes_ok(rows, d, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
+  if (ld_x < (columns ? rows : d)) return stage_error(GNNSTAGE_EINVAL, me + (columns ? "ld_x is below rows" : "ld_x is below d"));
+  if (rows == 0) return GNNSTAGE_OK;
+  if (!matrix_ok(x, dtype, err) || !stored_ok(q, ld_q, scale, ld_s, d, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const int e = dtype == GNNSTAGE_BF16 ? run_store(static_cast<const bf16_t *>(x), ld_x, rows, d, columns, q, ld_q, scale, ld_s, s)
+                                       : run_store(static_cast<const float *>(x), ld_x, rows, d, columns, q, ld_q, scale, ld_s, s);
+  if (e != hipSuccess) return stage_error(GNNSTAGE_EHIP, me + hipGetErrorString((hipError_t)e));
+  return GNNSTAGE_OK;
+}
+
+}  // namespace
+
+extern "C" int gnnstage_rows4_store(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t d, uint8_t *q, int64_t ld_q, uint8_t *scale, int64_t ld_s,
+                                    void *hip_stream) try {
+  return store("gnnstage_rows4_store", false, x, dtype, ld_x, rows, d, q, ld_q, scale, ld_s, hip_stream);
+}
+GNNSTAGE_GUARD_INT
+
+extern "C" int gnnstage_rows4_store_columns(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t d, uint8_t *q, int64_t ld_q, uint8_t *scale,
+                                            int64_t ld_s, void *hip_stream) try {
+  return store("gnnstage_rows4_store_columns", true, x, dtype, ld_x, rows, d, q, ld_q, scale, ld_s, hip_stream);
+}
+GNNSTAGE_GUARD_INT
+
+extern "C" int gnnstage_rows4_load(const uint8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, int64_t rows, int32_t d, void *x, int32_t dtype, int64_t ld_x,
+                                   void *hip_stream) try {
+  const std::string me = "gnnstage_rows4_load: ";
+  std::string err;
+  if (dtype != GNNSTAGE_F32 && dtype != GNNSTAGE_BF16) return stage_error(GNNSTAGE_EINVAL, me + "unknown dtype");
+  if (!sizes_ok(rows, d, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
+  if (ld_x < d) return stage_error(GNNSTAGE_EINVAL, me + "ld_x is below d");
+  if (rows == 0) return GNNSTAGE_OK;
+  if (!matrix_ok(x, dtype, err) || !stored_ok(q, ld_q, scale, ld_s, d, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
+  const int per_row = (d + 7) / 8;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const int e = for_row_slabs(rows, per_row, [&](int64_t r, int64_t m, unsigned gx) {
+    if (dtype == GNNSTAGE_BF16)
+      hipLaunchKernelGGL(rows4_load_kernel<bf16_t>, dim3(gx), dim3(256), 0, s, q + (size_t)(r * ld_q), ld_q, scale + (size_t)(r * ld_s), ld_s, m, d, per_row,
+                         static_cast<bf16_t *>(x) + (size_t)(r * ld_x), ld_x);
+    else
+      hipLaunchKernelGGL(rows4_load_kernel<float>, dim3(gx), dim3(256), 0, s, q + (size_t)(r * ld_q), ld_q, scale + (size_t)(r * ld_s), ld_s, m, d, per_row,
+                         static_cast<float *>(x) + (size_t)(r * ld_x), ld_x);
+  });
+  if (e != hipSuccess) return stage_error(GNNSTAGE_EHIP, me + hipGetErrorString((hipError_t)e));
+  return GNNSTAGE_OK;
+}
+GNNSTAGE_GUARD_INT
+
+extern "C" int gnnstage_rows4_product(const uint8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, int64_t rows, const uint8_t *other_q, int64_t ld_oq,
+                                      const uint8_t *other_scale, int64_t ld_os, int64_t others, int32_t d, const float *bias, void *out, int32_t dtype, int64_t ld_out,
+                                      void *hip_stream) try {
+  const std::string me = "gnnstage_rows4_product: ";
+  std::string err;
+  if (dtype != GNNSTAGE_F32 && dtype != GNNSTAGE_BF16) return stage_error(GNNSTAGE_EINVAL, me + "unknown dtype");
+  if (!sizes_ok(rows, d, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
+  if (others < 0 || others > ((int64_t)1 << 29)) return stage_error(GNNSTAGE_EINVAL, me + "others must be in [0, 2^29]");
+  if (ld_out < others) return stage_error(GNNSTAGE_EINVAL, me + "ld_out is below others");
+  if (rows == 0 || others == 0) return GNNSTAGE_OK;
+  if (!matrix_ok(out, dtype, err) || !stored_ok(q, ld_q, scale, ld_s, d, err) || !stored_ok(other_q, ld_oq, other_scale, ld_os, d, err))
+    return stage_error(GNNSTAGE_EINVAL, me + err);
+  ProductArgs p{};
+  p.a = q;
+  p.a_scale = scale;
+  p.ld_a = ld_q;
+  p.ld_as = ld_s;
+  p.b = other_q;
+  p.b_scale = other_scale;
+  p.ld_b = ld_oq;
+  p.ld_bs = ld_os;
+  p.M = rows;
+  p.N = others;
+  p.blocks = (d + 31) / 32;
+  p.bias = bias;
+  p.out = out;
+  p.ld_out = ld_out;
+  const int e = dtype == GNNSTAGE_BF16 ? run_product<bf16_t>(p, static_cast<hipStream_t>(hip_stream)) : run_product<float>(p, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return stage_error(GNNSTAGE_EHIP, me + hipGetErrorString((hipError_t)e));
+  return GNNSTAGE_OK;
+}
+GNNSTAGE_GUARD_INT
