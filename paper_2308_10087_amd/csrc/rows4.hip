@@ -173,8 +173,9 @@ struct ProductArgs {
   const float *bias;  // by column of the result, or NULL
   void *out;
   int64_t ld_out;
-  int64_t row_tiles, tiles;
-  uint32_t per_xcd;
+  int32_t per;         // tiles of 32 rows a wave
+  int32_t side;        // waves of a workgroup side by side, 1 or 4; the others are below one another
+  uint32_t split_cols, xcd_cols, xcd_rows;  // an XCD's workgroups, and whether XCDs have columns of their own or rows
 };
 // Operands of a row: 256 columns at a time, eight blocks.  Matrix instructions take 64 columns, 32 from each half of the wave; here the lower half has the blocks
 // 0 .. 3, the upper one 4 .. 7, one per instruction: a lane's are 64 bytes side by side, and their factors one word, a byte for each instruction.
@@ -208,68 +209,78 @@ __device__ __forceinline__ f32x16 multiply(const Operand &a, const Operand &b, f
 
 constexpr int kAcross = 4;  // columns of the result a lane: 128 a wave
 
-// A wave per tile of 32 DOWN rows and 128 columns.  A lane's columns are side by side (column 4 l + t is the t-th instruction's l-th), so that rows are
-// written 256 (512) bytes at a time from the registers.  Register i of lane l: row 8 (i / 4) + 4 (l / 32) + i % 4.
-template <typename O, int DOWN>
-__global__ __launch_bounds__(256) void rows4_product_kernel(const ProductArgs p) {
+// A wave owns 128 columns and goes down `per` tiles of 32 rows.  A lane's columns are side by side (column 4 l + t is the t-th instruction's l-th), so that rows
+// are written 256 (512) bytes at a time from the registers.  Register i of lane l: row 8 (i / 4) + 4 (l / 32) + i % 4.
+// ONE: up to 256 columns of operands, those of the wave's columns stay in registers and the next rows' are on their way.
+template <typename O, bool ONE>
+__global__ __launch_bounds__(256, 2) void rows4_product_kernel(const ProductArgs p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, h = lane >> 5;
-  // an XCD has tiles that follow one another: the columns' operands are read once into one L2
-  const int64_t tile = ((int64_t)(blockIdx.x & 7) * p.per_xcd + (blockIdx.x >> 3)) * 4 + wave;
-  if (blockIdx.x >> 3 >= p.per_xcd || tile >= p.tiles) return;
-  const int64_t n0 = tile / p.row_tiles * (32 * kAcross), m0 = tile % p.row_tiles * (32 * DOWN);
-  f32x16 sum[DOWN][kAcross];
-#pragma unroll
-  for (int i = 0; i < DOWN; ++i)
-#pragma unroll
-    for (int t = 0; t < kAcross; ++t)
-#pragma unroll
-      for (int k = 0; k < 16; ++k) sum[i][t][k] = 0.f;
-  for (int block = 0; block < p.blocks; block += 8) {
-    Operand a[DOWN], b[kAcross];
-    // (past the last row or column: that one once more, whatever it gives is not written)
-#pragma unroll
-    for (int i = 0; i < DOWN; ++i) {
-      const int64_t m = min(m0 + 32 * i + l, p.M - 1);
-      a[i].load(p.a + (size_t)(m * p.ld_a), p.a_scale + (size_t)(m * p.ld_as), block + 4 * h, p.blocks);
-    }
+  // An XCD has a share of the columns (or rows) and goes through it along the rows: what is side by side in memory is written at about the same time, so
+  // that the lines that two workgroups share are whole when they leave the L2, and the columns' operands stay there.
+  const uint32_t xcd = blockIdx.x & 7, local = blockIdx.x >> 3, lr = local / p.xcd_cols, lc = local - lr * p.xcd_cols;
+  const uint32_t gc = p.split_cols ? xcd * p.xcd_cols + lc : lc, gr = p.split_cols ? lr : xcd * p.xcd_rows + lr;
+  const int64_t col_tile = (int64_t)gc * p.side + wave % p.side, tile0 = ((int64_t)gr * (4 / p.side) + wave / p.side) * p.per;
+  const int64_t n0 = col_tile * (32 * kAcross), tile1 = min(tile0 + p.per, (p.M + 31) / 32);
+  if (n0 >= p.N || tile0 >= tile1) return;
+  // (past the last row or column: that one once more, whatever it gives is not written)
+  auto load_a = [&](Operand &x, int64_t tile, int block) {
+    const int64_t m = min(tile * 32 + l, p.M - 1);
+    x.load(p.a + (size_t)(m * p.ld_a), p.a_scale + (size_t)(m * p.ld_as), block + 4 * h, p.blocks);
+  };
+  auto load_b = [&](Operand (&x)[kAcross], int block) {
 #pragma unroll
     for (int t = 0; t < kAcross; ++t) {
       const int64_t n = min(n0 + kAcross * l + t, p.N - 1);
-      b[t].load(p.b + (size_t)(n * p.ld_b), p.b_scale + (size_t)(n * p.ld_bs), block + 4 * h, p.blocks);
+      x[t].load(p.b + (size_t)(n * p.ld_b), p.b_scale + (size_t)(n * p.ld_bs), block + 4 * h, p.blocks);
     }
-#pragma unroll
-    for (int i = 0; i < DOWN; ++i)
-#pragma unroll
-      for (int t = 0; t < kAcross; ++t) {
-        sum[i][t] = multiply<0>(a[i], b[t], sum[i][t]);
-        sum[i][t] = multiply<1>(a[i], b[t], sum[i][t]);
-        sum[i][t] = multiply<2>(a[i], b[t], sum[i][t]);
-        sum[i][t] = multiply<3>(a[i], b[t], sum[i][t]);
-      }
-  }
+  };
+  Operand b[kAcross], a, next;
+  load_a(next, tile0, 0);
+  load_b(b, 0);
   const int64_t n = n0 + kAcross * l;
   const bool whole = n + kAcross <= p.N;
   float bias[kAcross];
 #pragma unroll
   for (int t = 0; t < kAcross; ++t) bias[t] = p.bias && n + t < p.N ? p.bias[n + t] : 0.f;
+  for (int64_t tile = tile0; tile < tile1; ++tile) {
+    f32x16 sum[kAcross];
 #pragma unroll
-  for (int i = 0; i < DOWN; ++i)
+    for (int t = 0; t < kAcross; ++t)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) sum[t][k] = 0.f;
+    if constexpr (ONE) {
+      a = next;
+      if (tile + 1 < tile1) load_a(next, tile + 1, 0);
+#pragma unroll
+      for (int t = 0; t < kAcross; ++t) sum[t] = multiply<3>(a, b[t], multiply<2>(a, b[t], multiply<1>(a, b[t], multiply<0>(a, b[t], sum[t]))));
+    } else {
+      for (int block = 0; block < p.blocks; block += 8) {
+        load_a(a, tile, block);
+        load_b(b, block);
+#pragma unroll
+        for (int t = 0; t < kAcross; ++t) sum[t] = multiply<3>(a, b[t], multiply<2>(a, b[t], multiply<1>(a, b[t], multiply<0>(a, b[t], sum[t]))));
+      }
+    }
+    const int64_t m0 = tile * 32 + 4 * h;
+    O *row = static_cast<O *>(p.out) + (size_t)(m0 * p.ld_out) + n;
+    const bool all = tile * 32 + 32 <= p.M;
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      const int64_t m = m0 + 32 * i + 8 * (k >> 2) + 4 * h + (k & 3);
-      if (m >= p.M) continue;
-      O *out = static_cast<O *>(p.out) + (size_t)(m * p.ld_out) + n;
+      const int down = 8 * (k >> 2) + (k & 3);
+      if (!all && m0 + down >= p.M) continue;
+      O *out = row + (size_t)(down * p.ld_out);
       if (whole) {
         typename std::conditional<sizeof(O) == 2, bf16x4_u, f32x4_u>::type v;
 #pragma unroll
-        for (int t = 0; t < kAcross; ++t) v[t] = (O)(sum[i][t][k] + bias[t]);
+        for (int t = 0; t < kAcross; ++t) v[t] = (O)(sum[t][k] + bias[t]);
         *reinterpret_cast<decltype(v) *>(out) = v;
       } else {
 #pragma unroll
         for (int t = 0; t < kAcross; ++t)
-          if (n + t < p.N) out[t] = (O)(sum[i][t][k] + bias[t]);
+          if (n + t < p.N) out[t] = (O)(sum[t][k] + bias[t]);
       }
     }
+  }
 }
 
 bool sizes_ok(int64_t rows, int d, std::string &err) {
@@ -308,13 +319,15 @@ int run_store(const T *x, int64_t ld, int64_t rows, int d, bool columns, uint8_t
   return hipSuccess;
 }
 
+constexpr int64_t kWaves = 8192;  // that a launch should have before they take more than a tile each: four rounds of two per SIMD
+constexpr int64_t kMostTiles = 8;
 template <typename O>
 int run_product(ProductArgs p, hipStream_t s) {
-  const bool few = p.M <= 32;
-  const int down = few ? 32 : 64;
   const int64_t col_tiles = (p.N + 32 * kAcross - 1) / (32 * kAcross), rows = p.M;
+  p.side = col_tiles >= 4 ? 4 : 1;
+  const int64_t col_groups = (col_tiles + p.side - 1) / p.side;
   // as many rows as a launch takes workgroups for
-  const int64_t most = std::max<int64_t>(1, kMostBlocks / 2 * 4 / col_tiles) * down;
+  const int64_t most = std::max<int64_t>(1, kMostBlocks / 2 / col_groups) * 32;
   const uint8_t *a = p.a, *a_scale = p.a_scale;
   O *out = static_cast<O *>(p.out);
   for (int64_t r = 0; r < rows; r += most) {
@@ -322,11 +335,13 @@ int run_product(ProductArgs p, hipStream_t s) {
     p.a = a + (size_t)(r * p.ld_a);
     p.a_scale = a_scale + (size_t)(r * p.ld_as);
     p.out = out + (size_t)(r * p.ld_out);
-    p.row_tiles = (p.M + down - 1) / down;
-    p.tiles = p.row_tiles * col_tiles;
-    const int64_t groups = (p.tiles + 3) / 4;
-    p.per_xcd = (uint32_t)((groups + 7) / 8);
-    hipLaunchKernelGGL((few ? rows4_product_kernel<O, 1> : rows4_product_kernel<O, 2>), dim3(p.per_xcd * 8), dim3(256), 0, s, p);
+    const int64_t row_tiles = (p.M + 31) / 32;
+    p.per = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kMostTiles, row_tiles * col_tiles / kWaves));
+    const int64_t row_groups = (row_tiles + (int64_t)p.per * (4 / p.side) - 1) / ((int64_t)p.per * (4 / p.side));
+    p.split_cols = col_groups >= 16;
+    p.xcd_cols = (uint32_t)(p.split_cols ? (col_groups + 7) / 8 : col_groups);
+    p.xcd_rows = (uint32_t)(p.split_cols ? row_groups : (row_groups + 7) / 8);
+    hipLaunchKernelGGL((p.blocks <= 8 ? rows4_product_kernel<O, true> : rows4_product_kernel<O, false>), dim3(p.xcd_cols * p.xcd_rows * 8), dim3(256), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }
