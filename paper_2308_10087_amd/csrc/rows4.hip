@@ -27,74 +27,148 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
 typedef bf16_t bf16x8_u __attribute__((ext_vector_type(8), aligned(2)));
 typedef bf16_t bf16x4_u __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_u __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32_u __attribute__((aligned(1)));
 
-// columns c .. c + 7 of a row; zeros from d on
-template <typename T>
-__device__ inline void load8(const T *row, int c, int d, float (&v)[8]) {
-  if (c + 8 <= d) {
-    if constexpr (sizeof(T) == 2) {
-      const bf16x8_u x = *reinterpret_cast<const bf16x8_u *>(row + c);
-#pragma unroll
-      for (int t = 0; t < 8; ++t) v[t] = (float)x[t];
-    } else {
-      const f32x4_u x = *reinterpret_cast<const f32x4_u *>(row + c), y = *reinterpret_cast<const f32x4_u *>(row + c + 4);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        v[t] = x[t];
-        v[4 + t] = y[t];
-      }
-    }
-  } else {
-#pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = c + t < d ? (float)row[c + t] : 0.f;
-  }
-}
+typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
-// The factor of a block whose largest magnitude has the bits a: its byte, and 2^-e (0: not finite).
-__device__ __forceinline__ uint32_t factor_of(uint32_t a, float &inv) {
-  if (a >= 0x7f800000u) {
-    inv = 0.f;
-    return 255;
+// Eight columns c .. c + 7 of a row, zeros from d on (the row's last eight are loaded where it ends: one vector load for every thread): their largest magnitude as the bits of a float (infinities and NaNs are above every number), and
+// their codes of x / 2^e, two an instruction, rounded to the nearest, to the even of two as near.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<float> {
+  float v[8];
+  __device__ __forceinline__ void load(const float *row, int c, int d) {
+    if (d < 8) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) v[t] = c + t < d ? row[c + t] : 0.f;
+      return;
+    }
+    const int at = min(c, d - 8);
+    const f32x4_u x = *reinterpret_cast<const f32x4_u *>(row + at), y = *reinterpret_cast<const f32x4_u *>(row + at + 4);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      v[t] = x[t];
+      v[4 + t] = y[t];
+    }
   }
+  // moves what was loaded from further to the left, where the row ends, to its place
+  __device__ __forceinline__ void settle(int c, int d) {
+    const int n = c - (d - 8);
+    if (d < 8 || n <= 0) return;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = n & 1 ? (t < 7 ? v[t + (t < 7)] : 0.f) : v[t];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = n & 2 ? (t < 6 ? v[t + 2 * (t < 6)] : 0.f) : v[t];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = n & 4 ? (t < 4 ? v[t + 4 * (t < 4)] : 0.f) : v[t];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = n >= 8 ? 0.f : v[t];
+  }
+  __device__ __forceinline__ uint32_t largest() const {
+    uint32_t a = 0;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) a = max(a, __builtin_bit_cast(uint32_t, v[t]) & 0x7fffffffu);
+    return a;
+  }
+  __device__ __forceinline__ uint32_t codes(float factor) const {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], factor, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], factor, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], factor, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], factor, 3);
+  }
+};
+template <>
+struct Eight<bf16_t> {
+  uint32_t v[4];
+  __device__ __forceinline__ void load(const bf16_t *row, int c, int d) {
+    if (d < 8) {
+      const uint16_t *x = reinterpret_cast<const uint16_t *>(row);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) v[t] = (c + 2 * t < d ? (uint32_t)x[c + 2 * t] : 0u) | (c + 2 * t + 1 < d ? (uint32_t)x[c + 2 * t + 1] << 16 : 0u);
+      return;
+    }
+    const u32x4_u x = *reinterpret_cast<const u32x4_u *>(row + min(c, d - 8));
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = x[t];
+  }
+  __device__ __forceinline__ void settle(int c, int d) {
+    const int n = c - (d - 8);
+    if (d < 8 || n <= 0) return;
+    const uint32_t half = n & 1 ? 16 : 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = __builtin_amdgcn_alignbit(t < 3 ? v[t + (t < 3)] : 0u, v[t], half);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = n & 2 ? (t < 3 ? v[t + (t < 3)] : 0u) : v[t];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = n & 4 ? (t < 2 ? v[t + 2 * (t < 2)] : 0u) : v[t];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = n >= 8 ? 0u : v[t];
+  }
+  __device__ __forceinline__ uint32_t largest() const {
+    u16x2 a = {0, 0};
+#pragma unroll
+    for (int t = 0; t < 4; ++t) a = __builtin_elementwise_max(a, __builtin_bit_cast(u16x2, v[t] & 0x7fff7fffu));
+    return (uint32_t)max(a[0], a[1]) << 16;
+  }
+  __device__ __forceinline__ uint32_t codes(float factor) const {
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, v[0]), factor, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, v[1]), factor, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, v[2]), factor, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, v[3]), factor, 3);
+  }
+};
+
+// The byte of the factor of a block whose largest magnitude has the bits a; 255: not finite
+__device__ __forceinline__ uint32_t byte_of(uint32_t a) {
   // a = f 2^(E - 127) <= 7 2^e = 1.75 2^(2 + e): e = E - 129 up to f = 1.75, one more beyond
   const int e = min(max((int)(a >> 23) - 129 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0), -120), 125);
-  inv = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
-  return (uint32_t)(e + 127);
+  return a >= 0x7f800000u ? 255u : (uint32_t)(e + 127);
 }
-// The code of x / 2^e.  In the binades [0, 2), [2, 4), [4, 8) numbers are 1/2, 1, 2 apart: added to 1.5 2^23 times that the value is rounded to one of them,
-// to the even of two as near, which is the even code.
-__device__ __forceinline__ uint32_t code_of(float x, float inv) {
-  const float y = fabsf(x) * inv;
-  const float grid = y < 2.f ? 6291456.f : y < 4.f ? 12582912.f : 25165824.f;
-  const uint32_t from = y < 2.f ? 0u : y < 4.f ? 2u : 4u;
-  const uint32_t n = __builtin_bit_cast(uint32_t, y + grid) & 0xfu;
-  return min(n + from, 7u) | ((__builtin_bit_cast(uint32_t, x) >> 28) & 8u);
+__device__ __forceinline__ float factor_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }  // 255: infinity
+
+// Where a thread works: `across` threads (a row's, 256 of them at most) side by side, the rows below one another.  magic: thread / across as a product.
+struct Grid {
+  uint32_t across, down, magic;
+};
+Grid grid_of(int per_row) {
+  Grid g;
+  g.across = (uint32_t)std::min(per_row, 256);
+  g.down = 256 / g.across;
+  g.magic = 65536 / g.across + 1;  // (exact below 256)
+  return g;
 }
 
-// A thread per eight columns, four neighbouring lanes per block (quads never straddle rows: a row has whole blocks).
+// A thread per eight columns of kStoreRows rows, whose loads are on their way together; four neighbouring lanes per block (quads never straddle rows: a row has
+// whole blocks).
+constexpr int kStoreRows = 4;
 template <typename T>
-__global__ __launch_bounds__(256) void rows4_store_kernel(const T *x, int64_t ld, int64_t rows, int d, int blocks, uint8_t *q, int64_t ld_q, uint8_t *scale,
+__global__ __launch_bounds__(256) void rows4_store_kernel(const T *x, int64_t ld, int64_t rows, int d, int per_row, Grid at, uint8_t *q, int64_t ld_q, uint8_t *scale,
                                                           int64_t ld_s) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int per_row = blocks * 4;
-  const int64_t r = i / per_row;
-  if (r >= rows) return;
-  const int g = (int)(i - r * per_row), c = g * 8;
-  float v[8];
-  load8<T>(x + (size_t)(r * ld), c, d, v);
-  uint32_t a = 0;  // the largest magnitude, compared as bits: infinities and NaNs are above every number
+  const uint32_t y = threadIdx.x * at.magic >> 16;
+  const int64_t r0 = (int64_t)blockIdx.x * at.down * kStoreRows + y;
+  const int g = (int)(blockIdx.y * 256 + threadIdx.x - y * at.across);
+  if (y >= at.down || r0 >= rows || g >= per_row) return;  // whole quads
+  Eight<T> v[kStoreRows];
 #pragma unroll
-  for (int t = 0; t < 8; ++t) a = max(a, __builtin_bit_cast(uint32_t, v[t]) & 0x7fffffffu);
-  a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xf, 0xf, true));  // lanes 1 0 3 2 of the quad
-  a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x4E, 0xf, 0xf, true));  // lanes 2 3 0 1
-  float inv;
-  const uint32_t byte = factor_of(a, inv);
-  uint32_t w = 0;
+  for (int i = 0; i < kStoreRows; ++i) v[i].load(x + (size_t)(min(r0 + i * at.down, rows - 1) * ld), g * 8, d);
 #pragma unroll
-  for (int t = 0; t < 8; ++t) w |= (byte == 255 ? 0u : code_of(v[t], inv)) << (4 * t);
-  *reinterpret_cast<uint32_t *>(q + (size_t)(r * ld_q) + g * 4) = w;
-  if ((g & 3) == 0) scale[(size_t)(r * ld_s) + (g >> 2)] = (uint8_t)byte;
+  for (int i = 0; i < kStoreRows; ++i) {
+    const int64_t r = r0 + i * at.down;
+    v[i].settle(g * 8, d);
+    uint32_t a = v[i].largest();
+    a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0xB1, 0xf, 0xf, true));  // lanes 1 0 3 2 of the quad
+    a = max(a, (uint32_t)__builtin_amdgcn_mov_dpp((int)a, 0x4E, 0xf, 0xf, true));  // lanes 2 3 0 1
+    if (r >= rows) break;  // whole quads
+    const uint32_t byte = byte_of(a);
+    *reinterpret_cast<uint32_t *>(q + (size_t)(r * ld_q) + g * 4) = byte == 255 ? 0u : v[i].codes(factor_of(byte));
+    if ((g & 3) == 0) scale[(size_t)(r * ld_s) + (g >> 2)] = (uint8_t)byte;
+  }
 }
 
 // The columns of x (d x rows) as rows: a thread per block, 64 columns and four blocks down a workgroup.
@@ -104,55 +178,50 @@ __global__ __launch_bounds__(256) void rows4_store_columns_kernel(const T *x, in
   const int64_t r = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
   const int block = (int)blockIdx.y * 4 + (threadIdx.x >> 6);
   if (r >= rows || block >= blocks) return;
-  float v[32];
+  Eight<float> v[4];
   uint32_t a = 0;
 #pragma unroll
   for (int t = 0; t < 32; ++t) {
     const int k = block * 32 + t;
-    v[t] = k < d ? (float)x[(size_t)(k * ld) + r] : 0.f;
-    a = max(a, __builtin_bit_cast(uint32_t, v[t]) & 0x7fffffffu);
+    v[t >> 3].v[t & 7] = k < d ? (float)x[(size_t)(k * ld) + r] : 0.f;
   }
-  float inv;
-  const uint32_t byte = factor_of(a, inv);
-  uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int t = 0; t < 32; ++t) w[t >> 3] |= (byte == 255 ? 0u : code_of(v[t], inv)) << (4 * (t & 7));
-  *reinterpret_cast<u32x4 *>(q + (size_t)(r * ld_q) + block * 16) = u32x4{w[0], w[1], w[2], w[3]};
+  for (int i = 0; i < 4; ++i) a = max(a, v[i].largest());
+  const uint32_t byte = byte_of(a);
+  const float factor = factor_of(byte);
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = byte == 255 ? 0u : v[i].codes(factor);
+  *reinterpret_cast<u32x4 *>(q + (size_t)(r * ld_q) + block * 16) = w;
   scale[(size_t)(r * ld_s) + block] = (uint8_t)byte;
 }
 
 // A thread per eight columns
 template <typename T>
-__global__ __launch_bounds__(256) void rows4_load_kernel(const uint8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, int64_t rows, int d, int per_row, T *x,
-                                                         int64_t ld) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t r = i / per_row;
-  if (r >= rows) return;
-  const int g = (int)(i - r * per_row), c = g * 8;
+__global__ __launch_bounds__(256) void rows4_load_kernel(const uint8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, int64_t rows, int d, int per_row, Grid at,
+                                                         T *x, int64_t ld) {
+  const uint32_t y = threadIdx.x * at.magic >> 16;
+  const int64_t r = (int64_t)blockIdx.x * at.down + y;
+  const int g = (int)(blockIdx.y * 256 + threadIdx.x - y * at.across), c = g * 8;
+  if (y >= at.down || r >= rows || g >= per_row) return;
   const uint32_t w = *reinterpret_cast<const uint32_t *>(q + (size_t)(r * ld_q) + g * 4);
   const uint32_t byte = scale[(size_t)(r * ld_s) + (g >> 2)];
-  const float f = byte == 255 ? NAN : __builtin_bit_cast(float, byte << 23);
-  float v[8];
-#pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    const uint32_t code = w >> (4 * t), n = code & 7u;
-    // 1 + bit/2 in binade 2^(n / 2 - 1); the two below are 0 and 1/2
-    const float size = n < 2u ? 0.5f * (float)n : __builtin_bit_cast(float, ((n >> 1) + 126u) << 23 | (n & 1u) << 22);
-    v[t] = (code & 8u ? -size : size) * f;
-  }
+  const float f = byte == 255 ? NAN : factor_of(byte);
   T *row = x + (size_t)(r * ld) + c;
+  const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, f, 1), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, f, 2),
+                      __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, f, 3)};
   if (c + 8 <= d) {
     if constexpr (sizeof(T) == 2) {
       bf16x8_u o;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) o[t] = (bf16_t)v[t];
+      for (int t = 0; t < 8; ++t) o[t] = (bf16_t)v[t >> 1][t & 1];
       *reinterpret_cast<bf16x8_u *>(row) = o;
     } else {
       f32x4_u lo, hi;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        lo[t] = v[t];
-        hi[t] = v[4 + t];
+        lo[t] = v[t >> 1][t & 1];
+        hi[t] = v[2 + (t >> 1)][t & 1];
       }
       *reinterpret_cast<f32x4_u *>(row) = lo;
       *reinterpret_cast<f32x4_u *>(row + 4) = hi;
@@ -160,8 +229,20 @@ __global__ __launch_bounds__(256) void rows4_load_kernel(const uint8_t *q, int64
   } else {
 #pragma unroll
     for (int t = 0; t < 8; ++t)
-      if (c + t < d) row[t] = (T)v[t];
+      if (c + t < d) row[t] = (T)v[t >> 1][t & 1];
   }
+}
+// launch(first row, rows, workgroups down, workgroups across) for as many rows as a launch takes
+template <typename F>
+int for_grid_slabs(int64_t rows, int per_row, int64_t down, F launch) {
+  const int64_t gy = (per_row + 255) / 256, most = kMostBlocks / gy * down;
+  for (int64_t r = 0; r < rows; r += most) {
+    const int64_t m = std::min(most, rows - r);
+    launch(r, m, dim3((unsigned)((m + down - 1) / down), (unsigned)gy));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return (int)e;
+  }
+  return hipSuccess;
 }
 
 // ---- the product ----------------------------------------------------------------------------------------------------
@@ -303,9 +384,11 @@ bool matrix_ok(const void *x, int dtype, std::string &err) {
 template <typename T>
 int run_store(const T *x, int64_t ld, int64_t rows, int d, bool columns, uint8_t *q, int64_t ld_q, uint8_t *scale, int64_t ld_s, hipStream_t s) {
   const int blocks = (d + 31) / 32;
+  const Grid at = grid_of(blocks * 4);
   if (!columns)
-    return for_row_slabs(rows, blocks * 4, [&](int64_t r, int64_t m, unsigned gx) {
-      hipLaunchKernelGGL(rows4_store_kernel<T>, dim3(gx), dim3(256), 0, s, x + (size_t)(r * ld), ld, m, d, blocks, q + (size_t)(r * ld_q), ld_q, scale + (size_t)(r * ld_s), ld_s);
+    return for_grid_slabs(rows, blocks * 4, at.down * kStoreRows, [&](int64_t r, int64_t m, dim3 groups) {
+      hipLaunchKernelGGL(rows4_store_kernel<T>, groups, dim3(256), 0, s, x + (size_t)(r * ld), ld, m, d, blocks * 4, at, q + (size_t)(r * ld_q), ld_q, scale + (size_t)(r * ld_s),
+                         ld_s);
     });
   const int gy = (blocks + 3) / 4;
   const int64_t most = kMostBlocks / gy * 64;
@@ -389,12 +472,13 @@ extern "C" int gnnstage_rows4_load(const uint8_t *q, int64_t ld_q, const uint8_t
   if (!matrix_ok(x, dtype, err) || !stored_ok(q, ld_q, scale, ld_s, d, err)) return stage_error(GNNSTAGE_EINVAL, me + err);
   const int per_row = (d + 7) / 8;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const int e = for_row_slabs(rows, per_row, [&](int64_t r, int64_t m, unsigned gx) {
+  const Grid at = grid_of(per_row);
+  const int e = for_grid_slabs(rows, per_row, at.down, [&](int64_t r, int64_t m, dim3 groups) {
     if (dtype == GNNSTAGE_BF16)
-      hipLaunchKernelGGL(rows4_load_kernel<bf16_t>, dim3(gx), dim3(256), 0, s, q + (size_t)(r * ld_q), ld_q, scale + (size_t)(r * ld_s), ld_s, m, d, per_row,
+      hipLaunchKernelGGL(rows4_load_kernel<bf16_t>, groups, dim3(256), 0, s, q + (size_t)(r * ld_q), ld_q, scale + (size_t)(r * ld_s), ld_s, m, d, per_row, at,
                          static_cast<bf16_t *>(x) + (size_t)(r * ld_x), ld_x);
     else
-      hipLaunchKernelGGL(rows4_load_kernel<float>, dim3(gx), dim3(256), 0, s, q + (size_t)(r * ld_q), ld_q, scale + (size_t)(r * ld_s), ld_s, m, d, per_row,
+      hipLaunchKernelGGL(rows4_load_kernel<float>, groups, dim3(256), 0, s, q + (size_t)(r * ld_q), ld_q, scale + (size_t)(r * ld_s), ld_s, m, d, per_row, at,
                          static_cast<float *>(x) + (size_t)(r * ld_x), ld_x);
   });
   if (e != hipSuccess) return stage_error(GNNSTAGE_EHIP, me + hipGetErrorString((hipError_t)e));
