@@ -130,6 +130,8 @@ __device__ __forceinline__ Key sort_step(Key k) {  // blocks of N lanes, ordered
   return exchange<1>(k, down);
 }
 __device__ __forceinline__ Key sort_lanes(Key k) { return sort_step<64>(sort_step<32>(sort_step<16>(sort_step<8>(sort_step<4>(sort_step<2>(k)))))); }
+// 16 lanes whose eights are ordered down and up: all of them up
+__device__ __forceinline__ Key sort_sixteen_up(Key k) { return exchange<1>(exchange<2>(exchange<4>(exchange<8>(k, false), false), false), false); }
 // the 64 best of two ordered lists, in order; turned: the second one, from its last to its first
 __device__ __forceinline__ Key merge_lanes(Key list, Key turned) {
   Key k = exchange<32>(list > turned ? list : turned, true);
@@ -148,42 +150,93 @@ __device__ __forceinline__ void join_lanes(Sums &x) {
   join_across<32>(x);
 }
 
-constexpr int kWaiting = 128;  // room for keys that wait, per wave
+// the next number below; of minus infinity (and of NaN) there is none: NaN
+__device__ __forceinline__ float below(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  const uint32_t n = x > 0.f ? b - 1 : x < 0.f ? b + 1 : 0x80000001u;
+  return x > -INFINITY ? __builtin_bit_cast(float, n) : NAN;
+}
+
+#define LDS_AS __attribute__((address_space(3)))
+constexpr int kWaiting = 64 * 9;  // room for keys that wait, per wave: 63 and a step's
+// A logit is looked at unless it is at most the border: nothing is at most NaN.  Between two steps of a wave the border is the n_top-th best itself, since what comes
+// later and is equal is a higher class; within a step, and to the other waves of the row, the number below it.
 struct Best {
-  Key list;      // lane i: the i-th best
-  Key *waiting;  // LDS
-  int n, n_top;  // waiting; asked for
-  bool open;     // there are not n_top yet
-  float least;   // the n_top-th's logit
-  __device__ __forceinline__ Best(Key *room, int n_top) : list(0), waiting(room), n(0), n_top(n_top), open(true), least(-INFINITY) {}
-  __device__ __forceinline__ void merge() {
-    const int lane = threadIdx.x & 63;
-    __builtin_amdgcn_wave_barrier();
-    Key k = lane < n ? waiting[lane] : 0;
-    const Key rest = lane + 64 < n ? waiting[lane + 64] : 0;
-    __builtin_amdgcn_wave_barrier();
-    waiting[lane] = rest;
-    __builtin_amdgcn_wave_barrier();
-    n = max(n - 64, 0);
-    k = sort_lanes(k);
-    list = merge_lanes(list, lanes_at(k, 63 - lane));
-    const Key last = lanes_at(list, n_top - 1);
-    open = last == 0;
-    least = open ? -INFINITY : logit_of(last);
+  Key list;        // lane i: the i-th best
+  LDS_AS Key *waiting;
+  volatile LDS_AS float *borders;  // of the row's waves, where they share it (LDS has no NULL)
+  bool share;
+  int n, n_top;    // waiting; asked for
+  float least;     // the n_top-th's logit, NaN while there is none
+  float others, within;
+  float floor;     // a number that is below n_top others at least (and not one of them), NaN while none is known
+  __device__ __forceinline__ Best(Key *room, float *row_borders, bool share, int n_top)
+      : list(0), waiting((LDS_AS Key *)room), borders((LDS_AS float *)row_borders), share(share), n(0), n_top(n_top), least(NAN), others(NAN), within(NAN), floor(NAN) {}
+  // The border before a step, with what the row's other waves have found (whenever that was: what one of them has found is right for all)
+  __device__ __forceinline__ float border() {
+    if (share) {
+      others = fmaxf(fmaxf(borders[0], borders[1]), fmaxf(borders[2], borders[3]));
+    }
+    return fmaxf(fmaxf(least, floor), others);
   }
-  // a key per lane (0: none)
+  // and within it
+  __device__ __forceinline__ void enter() { within = fmaxf(fmaxf(below(least), floor), others); }
+  // The first whole step: of the lanes' largest logits the n_top-th is a number that n_top classes reach, so that not all of the step waits.
+  __device__ __forceinline__ void start(float most) {
+    if (n_top < 64) {
+      const Key kth = lanes_at(sort_lanes(key_of(most, threadIdx.x & 63)), n_top - 1);
+      floor = kth == 0 ? NAN : below(logit_of(kth));
+      tell(floor);
+    }
+  }
+  __device__ __forceinline__ void tell(float x) {
+    if (share && (threadIdx.x & 63) == 0) borders[threadIdx.x >> 6] = x;
+  }
+  // this lane's class c, where `in`
+  __device__ __forceinline__ void look(bool in, float z, int c) {
+    const bool mine = in && !(z <= within);
+    if (__ballot(mine) != 0) wait(mine ? key_of(z, c) : 0);
+  }
+  // a key per lane (0: none), 64 fewer than kWaiting before settle()
   __device__ __forceinline__ void wait(Key k) {
     const uint64_t votes = __ballot(k != 0);
-    if (votes == 0) return;
     if (k != 0) waiting[n + __popcll(votes & ((1ull << (threadIdx.x & 63)) - 1))] = k;
     n += __popcll(votes);
-    if (n >= 64) merge();
+  }
+  // as many as are merged in at once: few best are settled by few merges, but soon
+  __device__ __forceinline__ bool full() const { return n >= (n_top <= 16 ? 16 : 64); }
+  // merges all that waits in
+  __device__ __forceinline__ void settle() {
+    const int lane = threadIdx.x & 63;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    while (n > 0) {
+      Key last = lanes_at(list, n_top - 1);
+      if (n <= 16) {  // in the last lanes, from the least to the best
+        const int at = lane - 48;
+        Key k = at >= 0 && at < n ? waiting[at] : 0;
+        k = sort_step<8>(sort_step<4>(sort_step<2>(k)));
+        k = sort_sixteen_up(k);
+        n = 0;
+        list = merge_lanes(list, k);
+      } else {
+        const int at = n - 64 + lane;
+        const Key k = at >= 0 ? waiting[at] : 0;
+        n = max(n - 64, 0);
+        if (!__any(k > last)) continue;
+        list = merge_lanes(list, lanes_at(sort_lanes(k), 63 - lane));
+      }
+      last = lanes_at(list, n_top - 1);
+      least = last == 0 ? NAN : logit_of(last);
+      tell(fmaxf(below(least), floor));
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 };
 
 // ---- a wave's part of a row -----------------------------------------------------------------------------------------
 // Classes [c0, c1), the same for all lanes: what lies in front of the first 16-byte border a class per lane, whole vectors, what is left a class per lane.
-template <typename T, bool TOP>
+template <typename T, bool TOP, bool BIAS>
 __device__ __forceinline__ void scan(const T *row, const float *bias, int c0, int c1, int id, Sums &x, Best &best) {
   constexpr int N = kVec<T>;
   typedef typename Vec<T, N>::aligned_type TV;
@@ -202,9 +255,12 @@ __device__ __forceinline__ void scan(const T *row, const float *bias, int c0, in
 #pragma unroll
     for (int i = 1; i < N; ++i) most = fmaxf(most, z[i]);
     if constexpr (TOP) {
-      if (best.open || __any(most > best.least)) {
+      if (__any(!(most <= best.border()))) {
+        if (!(best.least == best.least) && !(best.floor == best.floor)) best.start(most);
+        best.enter();
 #pragma unroll
-        for (int i = 0; i < N; ++i) best.wait(in && (best.open || z[i] >= best.least) ? key_of(z[i], c + i) : 0);
+        for (int i = 0; i < N; ++i) best.look(in, z[i], c + i);
+        if (best.full()) best.settle();
       }
     }
     x.top = fmaxf(x.top, most);
@@ -218,8 +274,12 @@ __device__ __forceinline__ void scan(const T *row, const float *bias, int c0, in
   };
   auto single = [&](int c, bool in) {  // a class per lane
     float z = -INFINITY;
-    if (in) z = (float)row[c] + (bias ? bias[c] : 0.f);
-    if constexpr (TOP) best.wait(in && (best.open || z >= best.least) ? key_of(z, c) : 0);
+    if (in) z = (float)row[c] + (BIAS ? bias[c] : 0.f);
+    if constexpr (TOP) {
+      best.border();
+      best.enter();
+      best.look(in, z, c);
+    }
     x.top = fmaxf(x.top, z);
     if (__any(z > x.m + kFollow)) refer(x, fmaxf(x.m, z));
     add(c == id ? -INFINITY : z);
@@ -230,35 +290,36 @@ __device__ __forceinline__ void scan(const T *row, const float *bias, int c0, in
     BV b[N / 4];
   };
   const T *src = row + a0 + lane * N;
-  const float *bsrc = bias ? bias + a0 + lane * N : nullptr;
-  auto load = [&](Loaded &l, int v0) {
-    l.v = *reinterpret_cast<const TV *>(src + v0 * N);
-    if (bias) {
+  const float *bsrc = bias + a0 + lane * N;
+  auto load = [&](Loaded &l, int step) {
+    l.v = *reinterpret_cast<const TV *>(src + step * (64 * N));
+    if constexpr (BIAS) {
 #pragma unroll
-      for (int q = 0; q < N / 4; ++q) l.b[q] = *reinterpret_cast<const BV *>(bsrc + v0 * N + 4 * q);
+      for (int q = 0; q < N / 4; ++q) l.b[q] = *reinterpret_cast<const BV *>(bsrc + step * (64 * N) + 4 * q);
     }
   };
   auto open = [&](float (&z)[N], const Loaded &l) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) z[i] = (float)l.v[i];
-    if (bias) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) z[i] += l.b[i / 4][i % 4];
-    }
+    for (int i = 0; i < N; ++i) z[i] = BIAS ? (float)l.v[i] + l.b[i / 4][i % 4] : (float)l.v[i];
   };
-  // whole steps of all lanes, two on their way
+  // Whole steps of all lanes, in pairs; the next pair is on its way, without a branch (an access is waited for together with all in front of it): behind the last
+  // step that one again.
   const int steps = vectors / 64;
-  Loaded one, two;
-  if (steps > 0) load(one, 0);
-  for (int step = 0; step < steps; step += 2) {
-    float z[N];
-    if (step + 1 < steps) load(two, (step + 1) * 64);
-    open(z, one);
-    take(z, a0 + (step * 64 + lane) * N, a0 + step * 64 * N, true);
-    if (step + 1 < steps) {
-      if (step + 2 < steps) load(one, (step + 2) * 64);
-      open(z, two);
-      take(z, a0 + ((step + 1) * 64 + lane) * N, a0 + (step + 1) * 64 * N, true);
+  if (steps > 0) {
+    Loaded next[2];
+    load(next[0], 0);
+    load(next[1], min(1, steps - 1));
+    for (int step = 0; step < steps; step += 2) {
+      const Loaded now[2] = {next[0], next[1]};
+      load(next[0], min(step + 2, steps - 1));
+      load(next[1], min(step + 3, steps - 1));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (step + i >= steps) break;
+        float z[N];
+        open(z, now[i]);
+        take(z, a0 + ((step + i) * 64 + lane) * N, a0 + (step + i) * 64 * N, true);
+      }
     }
   }
   if (steps * 64 < vectors) {
@@ -268,8 +329,9 @@ __device__ __forceinline__ void scan(const T *row, const float *bias, int c0, in
 #pragma unroll
     for (int i = 0; i < N; ++i) z[i] = -INFINITY;
     if (in) {
-      load(one, steps * 64);
-      open(z, one);
+      Loaded l;
+      load(l, steps);
+      open(z, l);
     }
     take(z, a0 + v * N, a0 + steps * 64 * N, in);
   }
@@ -433,10 +495,11 @@ __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
 }
 
 // A wave per row (WAVES 1: four rows per workgroup), or a workgroup of four waves per row or part of one.
-template <typename T, bool TOP, int WAVES>
+template <typename T, bool TOP, bool BIAS, int WAVES>
 __global__ __launch_bounds__(256) void answer_kernel(const AnswerArgs a) {
   __shared__ Key room[TOP ? 4 * kWaiting : 1];
   __shared__ Sums met[4];
+  __shared__ float borders[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t r = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
   if (r >= a.rows) return;  // the whole wave (WAVES 1), nobody else's
@@ -447,16 +510,19 @@ __global__ __launch_bounds__(256) void answer_kernel(const AnswerArgs a) {
   const T *row = static_cast<const T *>(a.logits) + (size_t)(r * a.ld);
   const int id = given_class(a, r);
   Sums x = no_sums();
-  Best best(room + (TOP ? wave * kWaiting : 0), a.n_top);
+  Best best(room + (TOP ? wave * kWaiting : 0), borders, WAVES > 1, a.n_top);
   int c0 = 0, c1 = a.C;
   if constexpr (WAVES > 1) {
+    if constexpr (TOP) {
+      if (lane == 0) borders[wave] = NAN;
+      __syncthreads();
+    }
     const int begin = (int)blockIdx.y * a.part, end = min(a.C, begin + a.part), each = ((end - begin + 3) / 4 + 63) / 64 * 64;
     c0 = min(end, begin + wave * each);
     c1 = min(end, c0 + each);
   }
-  scan<T, TOP>(row, a.bias, c0, c1, id, x, best);
-  if constexpr (TOP)
-    if (best.n > 0) best.merge();
+  scan<T, TOP, BIAS>(row, a.bias, c0, c1, id, x, best);
+  if constexpr (TOP) best.settle();
   join_lanes(x);
   if constexpr (WAVES > 1) {
     if constexpr (TOP) room[wave * kWaiting + lane] = best.list;
@@ -485,6 +551,7 @@ __global__ __launch_bounds__(256) void answer_kernel(const AnswerArgs a) {
 template <typename T, bool TOP>
 __global__ __launch_bounds__(64) void answer_join_kernel(const AnswerArgs a) {
   __shared__ Key room[TOP ? kWaiting : 1];
+  __shared__ float unused[1];
   const int lane = threadIdx.x;
   const int64_t r = blockIdx.x;
   if (a.mask && a.mask[r] == 0) return;  // written
@@ -496,14 +563,15 @@ __global__ __launch_bounds__(64) void answer_join_kernel(const AnswerArgs a) {
   const Answer w = end_row(x, id >= 0, given_logit(a, row, id));
   if (lane == 0) write_row(a, r, w);
   if constexpr (TOP) {
-    Best best(room, a.n_top);
+    Best best(room, unused, false, a.n_top);
     const int n = a.n_top * a.splits;
     for (int i0 = 0; i0 < n; i0 += 64) {
       const Key k = i0 + lane < n ? a.part_keys[r * n + i0 + lane] : 0;
       // (of equal logits the lower class may come later here)
-      best.wait(k != 0 && (best.open || logit_of(k) >= best.least) ? k : 0);
+      best.wait(k != 0 && !(logit_of(k) < best.least) ? k : 0);
+      if (best.full()) best.settle();
     }
-    if (best.n > 0) best.merge();
+    best.settle();
     if (lane < a.n_top) write_best(a, r, lane, best.list, w);
   }
 }
@@ -567,8 +635,8 @@ int run_answer(const AnswerArgs &a, const AnswerPlan &p, hipStream_t s) {
       else run(answer_short_kernel<T, 4, 64>);
     });
   }
-  if (a.C < kLong) return slabs(4, 256, [&](const AnswerArgs &b, unsigned gx) { hipLaunchKernelGGL((answer_kernel<T, TOP, 1>), dim3(gx), dim3(256), 0, s, b); });
-  const int e = slabs(1, 256, [&](const AnswerArgs &b, unsigned gx) { hipLaunchKernelGGL((answer_kernel<T, TOP, 4>), dim3(gx, (unsigned)p.splits), dim3(256), 0, s, b); });
+  if (a.C < kLong) return slabs(4, 256, [&](const AnswerArgs &b, unsigned gx) { hipLaunchKernelGGL((a.bias ? answer_kernel<T, TOP, true, 1> : answer_kernel<T, TOP, false, 1>), dim3(gx), dim3(256), 0, s, b); });
+  const int e = slabs(1, 256, [&](const AnswerArgs &b, unsigned gx) { hipLaunchKernelGGL((a.bias ? answer_kernel<T, TOP, true, 4> : answer_kernel<T, TOP, false, 4>), dim3(gx, (unsigned)p.splits), dim3(256), 0, s, b); });
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL((answer_join_kernel<T, TOP>), dim3((unsigned)a.rows), dim3(64), 0, s, a);
   return (int)hipGetLastError();
