@@ -445,17 +445,13 @@ __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
 #pragma unroll
   for (int i = 0; i < N; ++i) x.top = fmaxf(x.top, z[i]);
   auto most_of = [&](float v) {
-    if constexpr (LANES == 4) {
-      v = fmaxf(v, lanes_xor<1>(v));
-      v = fmaxf(v, lanes_xor<2>(v));
-    }
+    if constexpr (LANES >= 2) v = fmaxf(v, lanes_xor<1>(v));
+    if constexpr (LANES >= 4) v = fmaxf(v, lanes_xor<2>(v));
     return v;
   };
   auto sum_of = [&](float v) {
-    if constexpr (LANES == 4) {
-      v += lanes_xor<1>(v);
-      v += lanes_xor<2>(v);
-    }
+    if constexpr (LANES >= 2) v += lanes_xor<1>(v);
+    if constexpr (LANES >= 4) v += lanes_xor<2>(v);
     return v;
   };
   x.top = most_of(x.top);
@@ -483,10 +479,8 @@ __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
     int c = N * LANES;
 #pragma unroll
     for (int i = N - 1; i >= 0; --i) c = z[i] == v ? sub + i * LANES : c;
-    if constexpr (LANES == 4) {
-      c = min(c, (int)lanes_xor<1>((uint32_t)c));
-      c = min(c, (int)lanes_xor<2>((uint32_t)c));
-    }
+    if constexpr (LANES >= 2) c = min(c, (int)lanes_xor<1>((uint32_t)c));
+    if constexpr (LANES >= 4) c = min(c, (int)lanes_xor<2>((uint32_t)c));
     if (sub == 0) {
       if (c < C) mine_at[c] = NAN;
       write_best(a, r, n, c < C ? key_of(v, c) : 0, w);
@@ -579,6 +573,7 @@ __global__ __launch_bounds__(64) void answer_join_kernel(const AnswerArgs a) {
 constexpr int kMostTop = 64;
 // Classes of a row that goes through LDS (answer_short_kernel); beyond 64 with few best classes only, each of which goes over all of the row.
 constexpr int kShort = 256, kShortTop = 8;
+constexpr int kLanes = 2;  // of a row of at most 64 classes
 constexpr int kLong = 4096;         // classes from which a row is a workgroup's
 constexpr int kWorkgroups = 512;    // that a launch should have: fewer rows are cut
 constexpr int kLeastPart = 2048;    // classes of a part
@@ -625,12 +620,12 @@ int run_answer(const AnswerArgs &a, const AnswerPlan &p, hipStream_t s) {
     return (int)hipSuccess;
   };
   if (a.C <= kShort && (a.C <= 64 || a.n_top <= kShortTop) && a.ld < 1 << 24) {  // (64 rows' places fit 32 bits)
-    return slabs(a.C <= 64 ? 64 : 16, 64, [&](const AnswerArgs &b, unsigned gx) {
+    return slabs(a.C <= 64 ? 64 / kLanes : 16, 64, [&](const AnswerArgs &b, unsigned gx) {
       auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(gx), dim3(64), 0, s, b); };
-      if (a.C <= 16) run(answer_short_kernel<T, 1, 16>);
-      else if (a.C <= 32) run(answer_short_kernel<T, 1, 32>);
-      else if (a.C <= 48) run(answer_short_kernel<T, 1, 48>);
-      else if (a.C <= 64) run(answer_short_kernel<T, 1, 64>);
+      if (a.C <= 16) run(answer_short_kernel<T, kLanes, 16 / kLanes>);
+      else if (a.C <= 32) run(answer_short_kernel<T, kLanes, 32 / kLanes>);
+      else if (a.C <= 48) run(answer_short_kernel<T, kLanes, 48 / kLanes>);
+      else if (a.C <= 64) run(answer_short_kernel<T, kLanes, 64 / kLanes>);
       else if (a.C <= 128) run(answer_short_kernel<T, 4, 32>);
       else run(answer_short_kernel<T, 4, 64>);
     });
