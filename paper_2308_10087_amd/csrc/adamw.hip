@@ -242,7 +242,7 @@ std::string adamw_check(const gnntrain_adamw_tensor *t, int n, int bits) {
     if (x.count < 0 || x.count > ((int64_t)1 << 35)) return bad("count must be in [0, 2^35]");
     if (x.count == 0) continue;
     if (!x.p || !x.g || !x.m || !x.v) return bad("p, g, m and v must not be NULL");
-    if ((x.g_dtype != GNNSTAGE_F32 && x.g_dtype != GNNSTAGE_BF16) || (x.compute_dtype != GNNSTAGE_F32 && x.compute_dtype != GNNSTAGE_BF16)) return bad("unknown dtype");
+    if ((x.g_dtype != GNNSTAGE_F32 && x.g_dtype != GNNSTAGE_BF16) || (x.compute && x.compute_dtype != GNNSTAGE_F32 && x.compute_dtype != GNNSTAGE_BF16)) return bad("unknown dtype");
     const uintptr_t g_align = x.g_dtype == GNNSTAGE_BF16 ? 1 : 3, c_align = x.compute && x.compute_dtype == GNNSTAGE_BF16 ? 1 : 3;
     if (((reinterpret_cast<uintptr_t>(x.p) | reinterpret_cast<uintptr_t>(x.m) | reinterpret_cast<uintptr_t>(x.v)) & 3) || (reinterpret_cast<uintptr_t>(x.g) & g_align) ||
         (reinterpret_cast<uintptr_t>(x.compute) & c_align))

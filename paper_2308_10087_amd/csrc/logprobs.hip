@@ -839,7 +839,7 @@ GradPlan grad_plan(int64_t rows, int C, int n) {
   p.across = std::min(256, (C + n - 1) / n);
   p.blocks = (C + p.across * n - 1) / (p.across * n);
   const int64_t down = 256 / p.across;
-  const int64_t most = std::max<int64_t>(1, kPartElements / C);
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kPartElements / C, kMostBlocks / 2 / p.blocks));
   // Workgroups that end soon keep in step with those beside them (rows of 200 KB at odd places, copied: 32 rows each 5.2 TB/s, 195 4.5), 2,048 of them at least.
   const int64_t few = std::max<int64_t>(kAhead * down, (rows * p.blocks + 2047) / 2048);
   p.rows_per = std::max<int64_t>(std::min<int64_t>(kChain * down, few), (rows + most - 1) / most);
