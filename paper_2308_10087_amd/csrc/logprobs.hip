@@ -383,7 +383,7 @@ __device__ __forceinline__ int given_class(const AnswerArgs &a, int64_t r) {
 }
 
 // Rows of few classes, at most N LANES: LANES (1 or 4) lanes each, with their logits in registers, so that what a row costs is its classes and not the lanes'
-// meetings.  A wave's rows go through LDS, kPitch floats apart: an odd number (LANES 1), or four times one, in which lanes meet in no bank.
+// meetings.  Bound by instructions in the chain of a wave's life, of which few are on a unit at a time (232,965 x 41 fp32, 3 best: 22 us, bytes 6).  A wave's rows go through LDS, kPitch floats apart: an odd number (LANES 1), or four times one, in which lanes meet in no bank.
 template <typename T, int LANES, int N>
 __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
   constexpr int kRows = 64 / LANES, kPitch = LANES * (N + 1);
@@ -488,7 +488,8 @@ __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
   }
 }
 
-// A wave per row (WAVES 1: four rows per workgroup), or a workgroup of four waves per row or part of one.
+// A wave per row (WAVES 1: four rows per workgroup), or a workgroup of four waves per row or part of one.  Bound by the vector units next to memory: a logit takes about ten
+// instructions and an exponential (8,191 x 100,003 bf16 with bias, ten best: 400 us, 4.1 TB/s; reads alone would take 268).
 template <typename T, bool TOP, bool BIAS, int WAVES>
 __global__ __launch_bounds__(256) void answer_kernel(const AnswerArgs a) {
   __shared__ Key room[TOP ? 4 * kWaiting : 1];
@@ -571,11 +572,16 @@ __global__ __launch_bounds__(64) void answer_join_kernel(const AnswerArgs a) {
 }
 
 constexpr int kMostTop = 64;
-// Classes of a row that goes through LDS (answer_short_kernel); beyond 64 with few best classes only, each of which goes over all of the row.
-constexpr int kShort = 256, kShortTop = 8;
-constexpr int kLanes = 2;  // of a row of at most 64 classes
-constexpr int kLong = 4096;         // classes from which a row is a workgroup's
-constexpr int kWorkgroups = 512;    // that a launch should have: fewer rows are cut
+// Rows of at most kShort classes go through LDS (answer_short_kernel), beyond 64 with at most kShortTop best classes, each of which goes over all of the row.  fp32, in us,
+// through LDS / a wave per row: 50,000 x 41, 3 best 13 / 58; x 64, 60 best 52 / 62; x 200, 8 best 31 / 54, 20 best 52 / 60, 32 best 75 / 65, 64 best 129 / 90.
+constexpr int kShort = 256, kShortTop = 24;
+constexpr int kLanes = 2;  // of a row of at most 64 classes (232,965 x 41, 3 best, 66 % of the rows: 1, 2, 4 lanes 25, 22, 25 us)
+// Others take a wave per row, or a workgroup where the classes are many and the rows few.  fp32, 5 best, in us, a wave / a workgroup: 600 x 4,000 14 / 13, 600 x 8,000
+// 19 / 13, 1,000 x 20,000 33 / 24, 1,000 x 100,003 125 / 75, 2,000 x 20,000 36 / 38, 2,000 x 100,003 151 / 149, 5,000 x 1,000 14 / 27, 5,000 x 8,000 34 / 48, 8,191 x 100,003 587 / 562 (bf16,
+// ten best, with bias 400 / 417).
+constexpr int kLong = 4096;
+constexpr int64_t kManyRows = 2048;
+constexpr int kWorkgroups = 512;    // that a launch of them should have: fewer rows are cut
 constexpr int kLeastPart = 2048;    // classes of a part
 
 struct AnswerPlan {
@@ -630,7 +636,7 @@ int run_answer(const AnswerArgs &a, const AnswerPlan &p, hipStream_t s) {
       else run(answer_short_kernel<T, 4, 64>);
     });
   }
-  if (a.C < kLong) return slabs(4, 256, [&](const AnswerArgs &b, unsigned gx) { hipLaunchKernelGGL((a.bias ? answer_kernel<T, TOP, true, 1> : answer_kernel<T, TOP, false, 1>), dim3(gx), dim3(256), 0, s, b); });
+  if (a.C < kLong || a.rows >= kManyRows) return slabs(4, 256, [&](const AnswerArgs &b, unsigned gx) { hipLaunchKernelGGL((a.bias ? answer_kernel<T, TOP, true, 1> : answer_kernel<T, TOP, false, 1>), dim3(gx), dim3(256), 0, s, b); });
   const int e = slabs(1, 256, [&](const AnswerArgs &b, unsigned gx) { hipLaunchKernelGGL((a.bias ? answer_kernel<T, TOP, true, 4> : answer_kernel<T, TOP, false, 4>), dim3(gx, (unsigned)p.splits), dim3(256), 0, s, b); });
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL((answer_join_kernel<T, TOP>), dim3((unsigned)a.rows), dim3(64), 0, s, a);
@@ -663,7 +669,8 @@ constexpr int kAhead = 4;       // rows of a thread on their way
 constexpr int kChain = 32;      // rows of a thread that dbias adds up in one chain, of which there is then one of their sums
 constexpr int kRowsAhead = 256;  // at most whose numbers are in LDS at a time
 
-// Workgroups own columns and go down their group's rows: the bias is read once per group, its gradient stays in registers.
+// Workgroups own columns and go down their group's rows: the bias is read once per group, its gradient stays in registers.  Bound by memory: 8,191 x 100,003 bf16 3.28 GB in 690 us,
+// 4.8 TB/s (rows of 200,006 bytes, whose lines two workgroups share; at whole lines a copy of this shape has 5.4).
 template <typename T, typename O, bool SUMS>
 __global__ __launch_bounds__(256) void grad_kernel(const GradArgs a) {
   constexpr int N = 16 / (sizeof(T) < sizeof(O) ? sizeof(O) : sizeof(T));

@@ -26,7 +26,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // rows start anywhere: the memory system takes vectors at any address of their elements
 typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
 typedef bf16_t bf16x8_u __attribute__((ext_vector_type(8), aligned(2)));
-typedef bf16_t bf16x4_u __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_u __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32_u __attribute__((aligned(1)));
 
@@ -146,7 +145,7 @@ Grid grid_of(int per_row) {
 
 // A thread per eight columns of kStoreRows rows, whose loads are on their way together; four neighbouring lanes per block (quads never straddle rows: a row has
 // whole blocks).
-constexpr int kStoreRows = 4;
+constexpr int kStoreRows = 4;  // 700,001 x 100 bf16, 187 MB: one row 57 us, four 38 (4.9 TB/s)
 template <typename T>
 __global__ __launch_bounds__(256) void rows4_store_kernel(const T *x, int64_t ld, int64_t rows, int d, int per_row, Grid at, uint8_t *q, int64_t ld_q, uint8_t *scale,
                                                           int64_t ld_s) {
@@ -196,7 +195,7 @@ __global__ __launch_bounds__(256) void rows4_store_columns_kernel(const T *x, in
   scale[(size_t)(r * ld_s) + block] = (uint8_t)byte;
 }
 
-// A thread per eight columns
+// A thread per eight columns.  Bound by memory: 700,001 x 100 to bf16, 187 MB in 31 us, 6.0 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void rows4_load_kernel(const uint8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_s, int64_t rows, int d, int per_row, Grid at,
                                                          T *x, int64_t ld) {
@@ -288,11 +287,12 @@ __device__ __forceinline__ f32x16 multiply(const Operand &a, const Operand &b, f
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a(S), b(S), c, 4, 4, S, (int)a.scale, S, (int)b.scale);  // 4: e2m1
 }
 
-constexpr int kAcross = 4;  // columns of the result a lane: 128 a wave
-
-// A wave owns 128 columns and goes down `per` tiles of 32 rows.  A lane's columns are side by side (column 4 l + t is the t-th instruction's l-th), so that rows
-// are written 256 (512) bytes at a time from the registers.  Register i of lane l: row 8 (i / 4) + 4 (l / 32) + i % 4.
+// A wave owns 32 kAcross columns and goes down `per` tiles of 32 rows.  A lane's columns are side by side (column kAcross l + t is the t-th instruction's l-th), so that
+// rows are written 256 (fp32: 512) bytes at a time from the registers.  Register i of lane l: row 8 (i / 4) + 4 (l / 32) + i % 4.
+// Bound by the results' writes: 8,191 x 100,003 x 256 to bf16 377 us, 4.3 TB/s (rows of 200,006 bytes: two workgroups share a line; at whole lines 5.4 - 5.9), matrix cores 0.2 of
+// the time; 3 x 400,009 x 256 by the other operands, 54 MB in 15 us.
 // ONE: up to 256 columns of operands, those of the wave's columns stay in registers and the next rows' are on their way.
+constexpr int kAcross = 4;
 template <typename O, bool ONE>
 __global__ __launch_bounds__(256, 2) void rows4_product_kernel(const ProductArgs p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, h = lane >> 5;
@@ -316,8 +316,10 @@ __global__ __launch_bounds__(256, 2) void rows4_product_kernel(const ProductArgs
     }
   };
   Operand b[kAcross], a, next;
-  load_a(next, tile0, 0);
-  load_b(b, 0);
+  if constexpr (ONE) {
+    load_a(next, tile0, 0);
+    load_b(b, 0);
+  }
   const int64_t n = n0 + kAcross * l;
   const bool whole = n + kAcross <= p.N;
   float bias[kAcross];
@@ -351,10 +353,11 @@ __global__ __launch_bounds__(256, 2) void rows4_product_kernel(const ProductArgs
       if (!all && m0 + down >= p.M) continue;
       O *out = row + (size_t)(down * p.ld_out);
       if (whole) {
-        typename std::conditional<sizeof(O) == 2, bf16x4_u, f32x4_u>::type v;
+        typedef O vector __attribute__((ext_vector_type(kAcross), aligned(sizeof(O))));
+        vector v;
 #pragma unroll
         for (int t = 0; t < kAcross; ++t) v[t] = (O)(sum[t][k] + bias[t]);
-        *reinterpret_cast<decltype(v) *>(out) = v;
+        *reinterpret_cast<vector *>(out) = v;
       } else {
 #pragma unroll
         for (int t = 0; t < kAcross; ++t)
@@ -403,6 +406,7 @@ int run_store(const T *x, int64_t ld, int64_t rows, int d, bool columns, uint8_t
 }
 
 constexpr int64_t kWaves = 8192;  // that a launch should have before they take more than a tile each: four rounds of two per SIMD
+// (8,191 x 100,003 x 256, 1 / 2 / 4 / 8 / 16 / 32 tiles a wave: 686 / 525 / 411 / 391 / 454 / 471 us: fewer load the columns' operands more often, more get out of step)
 constexpr int64_t kMostTiles = 8;
 template <typename O>
 int run_product(ProductArgs p, hipStream_t s) {
@@ -424,7 +428,8 @@ int run_product(ProductArgs p, hipStream_t s) {
     p.split_cols = col_groups >= 16;
     p.xcd_cols = (uint32_t)(p.split_cols ? (col_groups + 7) / 8 : col_groups);
     p.xcd_rows = (uint32_t)(p.split_cols ? row_groups : (row_groups + 7) / 8);
-    hipLaunchKernelGGL((p.blocks <= 8 ? rows4_product_kernel<O, true> : rows4_product_kernel<O, false>), dim3(p.xcd_cols * p.xcd_rows * 8), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((p.blocks <= 8 ? rows4_product_kernel<O, true> : rows4_product_kernel<O, false>),
+                       dim3(p.xcd_cols * p.xcd_rows * 8), dim3(256), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }
