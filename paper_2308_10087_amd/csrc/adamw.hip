@@ -149,14 +149,10 @@ __device__ __forceinline__ uint32_t encode4(f32x4 four, const uint32_t (&u)[4], 
   return w;
 }
 
-// Workgroups go through 1,024 kIter elements of one tensor each.  Bound by memory: 25.9 M elements with fp32 states and a bf16 copy (0.79 GB) 138 us, 5.7 TB/s; 102.6 M with states
-// in 8 bits and bf16 gradients (1.66 GB) 5.2 TB/s, next to about 100 vector instructions an element.  18 small tensors 4.5 us, where a launch each takes 2 - 3.
-// Four parts each have four times the loads in flight, which pays where an element's states are many bytes.  2^26 elements, 1 / 4 parts: fp32 356 / 347 us, 8 bits 193 / 208.
-template <int BITS>
-constexpr int kIter = BITS == 32 ? 4 : 1;
-template <int BITS>
+// Workgroups go through 1,024 ITER elements of one tensor each.  Bound by memory: 26.2 M elements with fp32 states and a bf16 copy (0.79 GB) 138 - 154 us, 5.1 - 5.7 TB/s; 102.7 M with
+// states in 8 bits and bf16 gradients (1.66 GB) 307 us, 5.4 TB/s, next to about 100 vector instructions an element.
+template <int BITS, int ITER>
 __global__ __launch_bounds__(256) void adamw_kernel(const Args a) {
-  constexpr int ITER = kIter<BITS>;
   // whose workgroup this is: a lane per tensor
   const int lane = threadIdx.x & 63;
   const int which = __popcll(__ballot(lane < kTensors && a.first[min(lane, kTensors - 1)] <= (int)blockIdx.x)) - 1;
@@ -228,6 +224,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Args a) {
   }
 }
 
+// Elements from which fp32 states take four parts a workgroup, which have four times the loads in flight.  In us, one part / four: 2^26 elements, fp32 356 / 347, 8 bits 193 / 208; 18
+// tensors of 276 k elements, fp32 4.5 / 9.0.
+constexpr int64_t kManyElements = 1 << 21;
+
 }  // namespace
 
 std::string adamw_check(const gnntrain_adamw_tensor *t, int n, int bits) {
@@ -287,7 +287,10 @@ int launch_adamw(const gnntrain_adamw_tensor *t, int n, int bits, const AdamwRat
   a.root_scale = (float)std::sqrt(1.0 / (1.0 - std::pow((double)r.beta2, (double)step)));
   a.eps = r.eps;
   const uint64_t base = mix(seed + (uint64_t)step * kGolden);
-  const int64_t per = 1024 * (bits == 32 ? kIter<32> : kIter<8>);
+  int64_t all = 0;
+  for (int i = 0; i < n; ++i) all += t[i].count;
+  const bool many = bits == 32 && all >= kManyElements;
+  const int64_t per = many ? 4096 : 1024;
   for (int i = 0; i < n;) {
     int k = 0;
     int64_t blocks = 0;
@@ -314,7 +317,7 @@ int launch_adamw(const gnntrain_adamw_tensor *t, int n, int bits, const AdamwRat
     }
     if (k == 0) break;
     for (; k < kTensors; ++k) a.first[k] = INT32_MAX;
-    hipLaunchKernelGGL((bits == 32 ? adamw_kernel<32> : adamw_kernel<8>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((bits == 8 ? adamw_kernel<8, 1> : many ? adamw_kernel<32, 4> : adamw_kernel<32, 1>), dim3((unsigned)blocks), dim3(256), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }

@@ -10,9 +10,10 @@
 // have no cancellation in rows that are sure of it.  A probability of zero contributes nothing to t (0 times minus infinity is no number).
 //
 // Best classes: a wave keeps the 64 best of what it has seen in its lanes, in order, as 64-bit keys (the logit's bits in the numbers' order, then the
-// class turned over, so that of equals the lower class is the larger key).  A logit has to be above the n_top-th of them to be looked at: one
-// comparison per vector.  Those that are wait in LDS until there are 64, which are sorted and merged in: a row of n logits in random order
-// has about 64 + n_top ln(n / 64) of them, two or three mergers.
+// class turned over, so that of equals the lower class is the larger key).  A logit has to be above a border to be looked at: one comparison per vector.  The border is what is
+// known to be below n_top others: the n_top-th of the first whole step's lanes' largest, then of the wave's list, or what another wave of the row has found.  Those that are above
+// wait in LDS until there are 16 (of more than 16 best: 64), which are sorted and merged in.  (Without the first step's border, and merged 64 at a time, 8,191 x 100,003 bf16 with
+// ten best took 26 % more vector instructions, 474 us for 417.)
 #include <hip/hip_runtime.h>
 #include "guard.h"
 
@@ -174,9 +175,7 @@ struct Best {
       : list(0), waiting((LDS_AS Key *)room), borders((LDS_AS float *)row_borders), share(share), n(0), n_top(n_top), least(NAN), others(NAN), within(NAN), floor(NAN) {}
   // The border before a step, with what the row's other waves have found (whenever that was: what one of them has found is right for all)
   __device__ __forceinline__ float border() {
-    if (share) {
-      others = fmaxf(fmaxf(borders[0], borders[1]), fmaxf(borders[2], borders[3]));
-    }
+    if (share) others = fmaxf(fmaxf(borders[0], borders[1]), fmaxf(borders[2], borders[3]));
     return fmaxf(fmaxf(least, floor), others);
   }
   // and within it
@@ -382,8 +381,9 @@ __device__ __forceinline__ int given_class(const AnswerArgs &a, int64_t r) {
   return (uint32_t)id < (uint32_t)a.C ? id : -1;
 }
 
-// Rows of few classes, at most N LANES: LANES (1 or 4) lanes each, with their logits in registers, so that what a row costs is its classes and not the lanes'
-// meetings.  Bound by instructions in the chain of a wave's life, of which few are on a unit at a time (232,965 x 41 fp32, 3 best: 22 us, bytes 6).  A wave's rows go through LDS, kPitch floats apart: an odd number (LANES 1), or four times one, in which lanes meet in no bank.
+// Rows of few classes, at most N LANES: LANES (2 or 4) lanes each, with their logits in registers, so that what a row costs is its classes and not the lanes'
+// meetings.  Bound by the chain of a wave's life: loads in three round trips, LDS, a search per best class (232,965 x 41 fp32, 3 best, 66 % of the rows: 22 us, the bytes alone 6).  A
+// wave's rows go through LDS, kPitch floats apart: LANES times an odd number, in which lanes meet in no bank.
 template <typename T, int LANES, int N>
 __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
   constexpr int kRows = 64 / LANES, kPitch = LANES * (N + 1);
