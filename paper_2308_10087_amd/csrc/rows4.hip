@@ -254,7 +254,7 @@ struct ProductArgs {
   void *out;
   int64_t ld_out;
   int32_t per;         // tiles of 32 rows a wave
-  int32_t side;        // waves of a workgroup side by side, 1 or 4; the others are below one another
+  int32_t side;        // waves of a workgroup side by side, all or one; the others are below one another
   uint32_t split_cols, xcd_cols, xcd_rows;  // an XCD's workgroups, and whether XCDs have columns of their own or rows
 };
 // Operands of a row: 256 columns at a time, eight blocks.  Matrix instructions take 64 columns, 32 from each half of the wave; here the lower half has the blocks
@@ -289,18 +289,19 @@ __device__ __forceinline__ f32x16 multiply(const Operand &a, const Operand &b, f
 
 // A wave owns 32 kAcross columns and goes down `per` tiles of 32 rows.  A lane's columns are side by side (column kAcross l + t is the t-th instruction's l-th), so that
 // rows are written 256 (fp32: 512) bytes at a time from the registers.  Register i of lane l: row 8 (i / 4) + 4 (l / 32) + i % 4.
-// Bound by the results' writes: 8,191 x 100,003 x 256 to bf16 377 us, 4.3 TB/s (rows of 200,006 bytes: two workgroups share a line; at whole lines 5.4 - 5.9), matrix cores 0.2 of
+// Bound by the results' writes: 8,191 x 100,003 x 256 to bf16 365 us, 4.5 TB/s (rows of 200,006 bytes: two workgroups share a line; at whole lines 5.4 - 5.9), matrix cores 0.2 of
 // the time; 3 x 400,009 x 256 by the other operands, 54 MB in 15 us.
 // ONE: up to 256 columns of operands, those of the wave's columns stay in registers and the next rows' are on their way.
 constexpr int kAcross = 4;
+constexpr int kGroup = 4;  // waves of a workgroup (2 / 4 / 8: 441 / 371 / 399 - 476 us)
 template <typename O, bool ONE>
-__global__ __launch_bounds__(256, 2) void rows4_product_kernel(const ProductArgs p) {
+__global__ __launch_bounds__(64 * kGroup, 2) void rows4_product_kernel(const ProductArgs p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, h = lane >> 5;
   // An XCD has a share of the columns (or rows) and goes through it along the rows: what is side by side in memory is written at about the same time, so
   // that the lines that two workgroups share are whole when they leave the L2, and the columns' operands stay there.
   const uint32_t xcd = blockIdx.x & 7, local = blockIdx.x >> 3, lr = local / p.xcd_cols, lc = local - lr * p.xcd_cols;
   const uint32_t gc = p.split_cols ? xcd * p.xcd_cols + lc : lc, gr = p.split_cols ? lr : xcd * p.xcd_rows + lr;
-  const int64_t col_tile = (int64_t)gc * p.side + wave % p.side, tile0 = ((int64_t)gr * (4 / p.side) + wave / p.side) * p.per;
+  const int64_t col_tile = (int64_t)gc * p.side + wave % p.side, tile0 = ((int64_t)gr * (kGroup / p.side) + wave / p.side) * p.per;
   const int64_t n0 = col_tile * (32 * kAcross), tile1 = min(tile0 + p.per, (p.M + 31) / 32);
   if (n0 >= p.N || tile0 >= tile1) return;
   // (past the last row or column: that one once more, whatever it gives is not written)
@@ -326,6 +327,8 @@ __global__ __launch_bounds__(256, 2) void rows4_product_kernel(const ProductArgs
 #pragma unroll
   for (int t = 0; t < kAcross; ++t) bias[t] = p.bias && n + t < p.N ? p.bias[n + t] : 0.f;
   for (int64_t tile = tile0; tile < tile1; ++tile) {
+    // (waves side by side have the same tiles, and stay in step: 391 -> 371 us at 8,191 x 100,003 x 256)
+    if (p.side == kGroup) __builtin_amdgcn_s_barrier();
     f32x16 sum[kAcross];
 #pragma unroll
     for (int t = 0; t < kAcross; ++t)
@@ -406,12 +409,12 @@ int run_store(const T *x, int64_t ld, int64_t rows, int d, bool columns, uint8_t
 }
 
 constexpr int64_t kWaves = 8192;  // that a launch should have before they take more than a tile each: four rounds of two per SIMD
-// (8,191 x 100,003 x 256, 1 / 2 / 4 / 8 / 16 / 32 tiles a wave: 686 / 525 / 411 / 391 / 454 / 471 us: fewer load the columns' operands more often, more get out of step)
+// (8,191 x 100,003 x 256, 4 / 6 / 8 / 10 / 16 tiles a wave: 409 / 379 / 371 / 376 / 407 us: fewer load the columns' operands more often, more get out of step)
 constexpr int64_t kMostTiles = 8;
 template <typename O>
 int run_product(ProductArgs p, hipStream_t s) {
   const int64_t col_tiles = (p.N + 32 * kAcross - 1) / (32 * kAcross), rows = p.M;
-  p.side = col_tiles >= 4 ? 4 : 1;
+  p.side = col_tiles >= kGroup ? kGroup : 1;
   const int64_t col_groups = (col_tiles + p.side - 1) / p.side;
   // as many rows as a launch takes workgroups for
   const int64_t most = std::max<int64_t>(1, kMostBlocks / 2 / col_groups) * 32;
@@ -424,12 +427,12 @@ int run_product(ProductArgs p, hipStream_t s) {
     p.out = out + (size_t)(r * p.ld_out);
     const int64_t row_tiles = (p.M + 31) / 32;
     p.per = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kMostTiles, row_tiles * col_tiles / kWaves));
-    const int64_t row_groups = (row_tiles + (int64_t)p.per * (4 / p.side) - 1) / ((int64_t)p.per * (4 / p.side));
+    const int64_t row_groups = (row_tiles + (int64_t)p.per * (kGroup / p.side) - 1) / ((int64_t)p.per * (kGroup / p.side));
     p.split_cols = col_groups >= 16;
     p.xcd_cols = (uint32_t)(p.split_cols ? (col_groups + 7) / 8 : col_groups);
     p.xcd_rows = (uint32_t)(p.split_cols ? row_groups : (row_groups + 7) / 8);
     hipLaunchKernelGGL((p.blocks <= 8 ? rows4_product_kernel<O, true> : rows4_product_kernel<O, false>),
-                       dim3(p.xcd_cols * p.xcd_rows * 8), dim3(256), 0, s, p);
+                       dim3(p.xcd_cols * p.xcd_rows * 8), dim3(64 * kGroup), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return (int)e;
   }
