@@ -382,45 +382,41 @@ __device__ __forceinline__ int given_class(const AnswerArgs &a, int64_t r) {
 }
 
 // Rows of few classes, at most N LANES: LANES (2 or 4) lanes each, with their logits in registers, so that what a row costs is its classes and not the lanes'
-// meetings.  Bound by the chain of a wave's life: loads in three round trips, LDS, a search per best class (232,965 x 41 fp32, 3 best, 66 % of the rows: 22 us, the bytes alone 6).  A
+// meetings.  Bound by the chain of a wave's life: loads in four round trips, LDS, a search per best class (232,965 x 41 fp32, 3 best, 66 % of the rows: 18 us, the bytes alone 6).  A
 // wave's rows go through LDS, kPitch floats apart: LANES times an odd number, in which lanes meet in no bank.
 template <typename T, int LANES, int N>
 __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
   constexpr int kRows = 64 / LANES, kPitch = LANES * (N + 1);
-  __shared__ float at[kRows * kPitch + 1];
+  __shared__ float at[kRows * kPitch];
   const int lane = threadIdx.x, mine = lane / LANES, sub = lane & (LANES - 1), C = a.C;
   const int64_t r0 = (int64_t)blockIdx.x * kRows, r = r0 + mine;
   const int rows = (int)min((int64_t)kRows, a.rows - r0);
   const bool on = mine < rows && (a.mask == nullptr || a.mask[r] != 0);
   const T *src = static_cast<const T *>(a.logits) + (size_t)(r0 * a.ld);
-  // The rows' classes one behind another, 64 at a time, without a branch: what is behind the last row is the first element over and over, and goes to a
-  // place of its own.  (Rows that take no part come along; whether they do would be asked per element.)
+  // Rows (of up to 32 classes: two or four of them) an instruction, a class per lane, without a branch: past the last row that one once more, which writes what is there; past
+  // the last class minus infinity, no class.  (Rows that take no part come along.)
   {
-    const int row = lane / C, n = rows * C, row_step = 64 / C, c_step = 64 - row_step * C;
-    int c = lane - row * C, to = row * kPitch + c;
-    uint32_t from = (uint32_t)(row * a.ld + c);
-    const uint32_t from_step = (uint32_t)(row_step * a.ld + c_step), from_over = (uint32_t)(a.ld - C);
-    constexpr int kAhead = 8;
-    for (int e0 = lane; e0 - lane < n; e0 += 64 * kAhead) {
-      T v[kAhead];
-      float b[kAhead];
-      int place[kAhead];
+    constexpr int W = N * LANES, kWide = W <= 16 ? 16 : W <= 32 ? 32 : 64, kOnce = 64 / kWide, kPieces = (W + 63) / 64, kBatch = kPieces == 1 ? 8 : 4;
+    static_assert(kRows % (kOnce * kBatch) == 0, "whole batches");
+    const int c = lane & (kWide - 1), y = lane / kWide;
+    float b[kPieces];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const bool ok = e0 + 64 * i < n;
-        place[i] = ok ? to : kRows * kPitch;
-        v[i] = src[ok ? from : 0u];
-        b[i] = a.bias ? a.bias[c] : 0.f;
-        c += c_step;
-        const bool over = c >= C;
-        c -= over ? C : 0;
-        from += from_step + (over ? from_over : 0u);
-        to += row_step * kPitch + c_step + (over ? kPitch - C : 0);
+    for (int q = 0; q < kPieces; ++q) b[q] = a.bias ? a.bias[min(c + 64 * q, C - 1)] : 0.f;
+#pragma unroll 1
+    for (int row0 = y; row0 < kRows; row0 += kOnce * kBatch) {
+      T v[kBatch][kPieces];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+        for (int q = 0; q < kPieces; ++q) v[i][q] = src[(uint32_t)(min(row0 + i * kOnce, rows - 1) * (int)a.ld) + (uint32_t)min(c + 64 * q, C - 1)];
+      if (c < W) {  // (of 48 classes' lanes the last 16 have no place)
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+          for (int q = 0; q < kPieces; ++q)
+            at[min(row0 + i * kOnce, rows - 1) * kPitch + c + 64 * q] = c + 64 * q < C ? (float)v[i][q] + b[q] + 0.f : -INFINITY;  // (minus zero is zero)
       }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) at[place[i]] = (float)v[i] + b[i] + 0.f;  // (minus zero is zero)
     }
-    for (int k = C + sub; k < N * LANES; k += LANES) at[mine * kPitch + k] = -INFINITY;  // no classes
   }
   __syncthreads();
   if (mine >= rows) return;  // all lanes of the row
@@ -575,7 +571,7 @@ constexpr int kMostTop = 64;
 // Rows of at most kShort classes go through LDS (answer_short_kernel), beyond 64 with at most kShortTop best classes, each of which goes over all of the row.  fp32, in us,
 // through LDS / a wave per row: 50,000 x 41, 3 best 13 / 58; x 64, 60 best 52 / 62; x 200, 8 best 31 / 54, 20 best 52 / 60, 32 best 75 / 65, 64 best 129 / 90.
 constexpr int kShort = 256, kShortTop = 24;
-constexpr int kLanes = 2;  // of a row of at most 64 classes (232,965 x 41, 3 best, 66 % of the rows: 1, 2, 4 lanes 25, 22, 25 us)
+constexpr int kLanes = 2;  // of a row of at most 64 classes (232,965 x 41, 3 best, 66 % of the rows: 1, 2, 4 lanes 25, 22, 25 us, with a place worked out per element)
 // Others take a wave per row, or a workgroup where the classes are many and the rows few.  fp32, 5 best, in us, a wave / a workgroup: 600 x 4,000 14 / 13, 600 x 8,000
 // 19 / 13, 1,000 x 20,000 33 / 24, 1,000 x 100,003 125 / 75, 2,000 x 20,000 36 / 38, 2,000 x 100,003 151 / 149, 5,000 x 1,000 14 / 27, 5,000 x 8,000 34 / 48, 8,191 x 100,003 587 / 562 (bf16,
 // ten best, with bias 400 / 417).
