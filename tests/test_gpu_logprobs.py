@@ -162,6 +162,32 @@ def test_orders_masks_and_numbers_at_the_edges(kind, C, dtype):
         _check(torch.from_numpy(z).to(DT[dtype]), None, ids, None, top, shift=1)
 
 
+@pytest.mark.parametrize("rows,C,top", [(2047, 4096, 3), (2048, 4096, 3), (2049, 5001, 64), (2050, 300, 25), (2500, 200, 24), (2500, 200, 25), (40, 257, 16), (40, 257, 17)])
+def test_both_sides_of_the_rules(rows, C, top):
+    logits, b, ids, mask = _inputs(rows, C, "f32", rows + C, True)
+    _check(logits, b, ids, mask, top, pad=1)
+
+
+@pytest.mark.parametrize("ld", [(1 << 24) - 1, 1 << 24])
+def test_short_rows_far_apart(ld):
+    """On both sides of what 32 bits hold of a row's place."""
+    g = _g()
+    rows, C = 40, 41
+    flat = torch.empty((rows - 1) * ld + C, dtype=torch.bfloat16, device=DEV)
+    view = torch.as_strided(flat, (rows, C), (ld, 1))
+    logits, b, ids, mask = _inputs(rows, C, "bf16", 3, True)
+    view.copy_(logits)
+    z = formula.logits_32(logits.float().numpy(), b)
+    w, on = formula.answer(z, ids), mask != 0
+    bound = formula.bounds(w, C)
+    logp, H, top_ids, top_logp = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty(rows, 4, dtype=torch.int32, device=DEV), torch.empty(rows, 4, device=DEV)
+    ws = torch.zeros(g.gnntrain_logprobs_workspace_size(rows, C, 4), dtype=torch.uint8, device=DEV)
+    g.gnntrain_logprobs(view, _dev(b), _dev(ids), _dev(mask), logp, H, None, ws, top_ids=top_ids, top_logp=top_logp)
+    _same(logp.cpu().numpy()[on], w["logp"][on], bound["logp"][on], "logp")
+    _same(H.cpu().numpy()[on], w["entropy"][on], bound["entropy"][on], "entropy")
+    assert np.array_equal(top_ids.cpu().numpy()[on], formula.best(z, 4)[on])
+
+
 def test_what_is_not_asked_for():
     g = _g()
     logits, b, ids, _ = _inputs(20, 100, "f32", 5)
