@@ -17,7 +17,7 @@ AT = (C.addressof(BUF) + 255) // 256 * 256  # never read
 
 def _tensor(k=0, **more):
     t = gnntrain_adamw_tensor()
-    values = dict(p=AT + 8192 * k, g=AT + 8192 * k + 1024, m=AT + 8192 * k + 2048, v=AT + 8192 * k + 3072, m_scale=AT + 8192 * k + 4096,
+    values = dict(p=AT + 8192 * k, g=AT + 8192 * k + 1000, m=AT + 8192 * k + 2000, v=AT + 8192 * k + 3000, m_scale=AT + 8192 * k + 4096,
                   v_scale=AT + 8192 * k + 4200, compute=None, count=100, g_dtype=0, compute_dtype=0, weight_decay=0.1)
     values.update(more)
     for name, x in values.items():
@@ -31,9 +31,9 @@ def _step(*tensors, bits=8, b1=0.9, b2=0.999, t=1, n=None):
 
 
 ONE = [dict(p=None), dict(g=None), dict(m=None), dict(v=None), dict(count=-1), dict(count=(1 << 35) + 1), dict(g_dtype=2), dict(compute=AT + 5000, compute_dtype=3),
-       dict(m_scale=None), dict(v_scale=None), dict(p=AT + 2), dict(g=AT + 1025), dict(m=AT + 2049), dict(compute=AT + 5001, compute_dtype=1),
-       dict(p=AT + 1024), dict(p=AT + 1020), dict(m=AT + 396), dict(v=AT + 2148 - 4), dict(compute=AT, compute_dtype=1), dict(compute=AT + 4, compute_dtype=0),
-       dict(m_scale=AT + 4200), dict(m_scale=AT + 4197), dict(v=AT + 2048)]
+       dict(m_scale=None), dict(v_scale=None), dict(p=AT + 2), dict(g=AT + 1001), dict(m=AT + 2001), dict(compute=AT + 5001, compute_dtype=1),
+       dict(p=AT + 1000), dict(p=AT + 996), dict(m=AT + 396), dict(v=AT + 2100 - 4), dict(compute=AT, compute_dtype=1), dict(compute=AT + 4, compute_dtype=0),
+       dict(m_scale=AT + 4200), dict(m_scale=AT + 4197), dict(v=AT + 2000)]
 
 
 @pytest.mark.parametrize("bad", ONE)
