@@ -59,7 +59,7 @@ struct Tensor {
 };
 struct Args {
   Tensor t[kTensors];
-  int32_t first[kTensors];  // workgroup; past the last tensor: beyond every one
+  int32_t first[kTensors];  // workgroup (negative: a tensor that the launch in front of this one began); past the last tensor: beyond every one
   const float *grad_scale;
   float b1, b2, a1, a2, rate, root_scale, eps;  // a = 1 - b, rate = lr c1, root_scale = sqrt(c2)
 };
@@ -291,29 +291,36 @@ int launch_adamw(const gnntrain_adamw_tensor *t, int n, int bits, const AdamwRat
   for (int i = 0; i < n; ++i) all += t[i].count;
   const bool many = bits == 32 && all >= kManyElements;
   const int64_t per = many ? 4096 : 1024;
+  int64_t done = 0;  // workgroups of tensor i in earlier launches
   for (int i = 0; i < n;) {
     int k = 0;
     int64_t blocks = 0;
-    for (; i < n && k < kTensors; ++i) {
+    while (i < n && k < kTensors && blocks < kMostBlocks) {
       const gnntrain_adamw_tensor &x = t[i];
-      if (x.count == 0) continue;
-      const int64_t b = (x.count + per - 1) / per;
-      if (blocks + b > kMostBlocks && k > 0) break;
-      Tensor &y = a.t[k];
-      y.p = x.p;
-      y.g = x.g;
-      y.m = x.m;
-      y.v = x.v;
-      y.m_scale = x.m_scale;
-      y.v_scale = x.v_scale;
-      y.compute = x.compute == x.p ? nullptr : x.compute;
-      y.n = x.count;
-      y.key = mix(base + (uint64_t)(i + 1) * kGolden);
-      y.keep = (float)(1.0 - (double)r.lr * (double)x.weight_decay);
-      y.g_bf16 = x.g_dtype == GNNSTAGE_BF16;
-      y.compute_bf16 = x.compute_dtype == GNNSTAGE_BF16;
-      a.first[k++] = (int32_t)blocks;
-      blocks += b;
+      const int64_t left = (x.count + per - 1) / per - done, b = std::min(left, kMostBlocks - blocks);
+      if (b > 0) {
+        Tensor &y = a.t[k];
+        y.p = x.p;
+        y.g = x.g;
+        y.m = x.m;
+        y.v = x.v;
+        y.m_scale = x.m_scale;
+        y.v_scale = x.v_scale;
+        y.compute = x.compute == x.p ? nullptr : x.compute;
+        y.n = x.count;
+        y.key = mix(base + (uint64_t)(i + 1) * kGolden);
+        y.keep = (float)(1.0 - (double)r.lr * (double)x.weight_decay);
+        y.g_bf16 = x.g_dtype == GNNSTAGE_BF16;
+        y.compute_bf16 = x.compute_dtype == GNNSTAGE_BF16;
+        a.first[k++] = (int32_t)(blocks - done);
+        blocks += b;
+      }
+      if (b < left) {  // the others are the next launch's
+        done += b;
+        break;
+      }
+      done = 0;
+      ++i;
     }
     if (k == 0) break;
     for (; k < kTensors; ++k) a.first[k] = INT32_MAX;
