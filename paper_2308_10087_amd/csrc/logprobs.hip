@@ -77,6 +77,14 @@ __device__ __forceinline__ Answer end_row(Sums x, bool given, float zl) {
   return a;
 }
 
+// Between what lanes of a wave write to LDS and what others of them read there.  LDS does a wave's instructions in their order; that the compiler keeps to it takes fences: a barrier
+// of the wave alone orders no accesses, and a lane that wrote nothing might go on with what it read before.  (No instructions of their own.)
+__device__ __forceinline__ void lds_written() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ---- the best classes -----------------------------------------------------------------------------------------------
 typedef uint64_t Key;  // 0: none
 __device__ __forceinline__ Key key_of(float z, int c) {
@@ -207,7 +215,7 @@ struct Best {
   // merges all that waits in
   __device__ __forceinline__ void settle() {
     const int lane = threadIdx.x & 63;
-    __builtin_amdgcn_wave_barrier();
+    lds_written();
 #pragma unroll 1
     while (n > 0) {
       Key last = lanes_at(list, n_top - 1);
@@ -229,7 +237,7 @@ struct Best {
       least = last == 0 ? NAN : logit_of(last);
       tell(fmaxf(below(least), floor));
     }
-    __builtin_amdgcn_wave_barrier();
+    lds_written();
   }
 };
 
@@ -434,7 +442,7 @@ __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
   };
   // (the row's lanes are of one wave, whose LDS instructions are done in their order)
   if (id >= 0 && sub == 0) mine_at[id] = -INFINITY;
-  __builtin_amdgcn_wave_barrier();
+  lds_written();
   read();
   Sums x = no_sums();
   x.top = id >= 0 ? zl : -INFINITY;
@@ -466,7 +474,7 @@ __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
   // The best, the lowest class that has it, which then is no number any more, and so on.
   if (id >= 0 && sub == 0) mine_at[id] = zl;
   for (int n = 0; n < a.n_top; ++n) {
-    __builtin_amdgcn_wave_barrier();
+    lds_written();
     read();
     float v = -INFINITY;
 #pragma unroll
