@@ -201,7 +201,7 @@ int gnntrain_adam_step(float *p, const float *g, float *m, float *v, void *compu
  * tensors: HOST, n of them, read during the call.  p (fp32), g (of g_dtype), compute (of compute_dtype, or NULL, or p): DEVICE, count elements, at any multiple of
  * their elements' size; m, v: DEVICE, count floats or bytes, at multiples of four bytes.  Buffers that are written may not overlap any other (gradients may
  * be shared).  count in [0, 2^35].  t = 1, 2, ...: a host number, as lr is, so that a captured call repeats its step.  grad_scale: DEVICE, one
- * float (what clips the gradients' norm, say), or NULL: 1.  beta1, beta2 in [0, 1).  Asynchronous, needs no workspace.
+ * float in no buffer that is written (what clips the gradients' norm, say), or NULL: 1.  beta1, beta2 in [0, 1).  Asynchronous, needs no workspace.
  * Message of an error: gnntrain_last_error(NULL). */
 typedef struct {
   float *p;

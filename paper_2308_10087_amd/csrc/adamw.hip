@@ -230,14 +230,14 @@ constexpr int64_t kManyElements = 1 << 21;
 
 }  // namespace
 
-std::string adamw_check(const gnntrain_adamw_tensor *t, int n, int bits) {
+std::string adamw_check(const gnntrain_adamw_tensor *t, int n, int bits, const float *grad_scale) {
   struct Range {
     uintptr_t from, to;
-    int tensor;
+    int tensor;  // -1: grad_scale
     bool written;
   };
   std::vector<Range> ranges;
-  ranges.reserve((size_t)n * 5);
+  ranges.reserve((size_t)n * 7 + 1);
   for (int i = 0; i < n; ++i) {
     const gnntrain_adamw_tensor &x = t[i];
     auto bad = [&](const char *why) { return "tensor " + std::to_string(i) + ": " + why; };
@@ -265,11 +265,20 @@ std::string adamw_check(const gnntrain_adamw_tensor *t, int n, int bits) {
     if (x.compute != x.p) add(x.compute, (x.compute_dtype == GNNSTAGE_BF16 ? 2 : 4) * c, true);
     else if (x.compute_dtype != GNNSTAGE_F32) return bad("compute is p, but not of its type");
   }
+  if (grad_scale) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(grad_scale);
+    if (at & 3) return "grad_scale is not aligned to its element";
+    ranges.push_back(Range{at, at + sizeof(float), -1, false});
+  }
   // no written buffer meets another one (gradients may be shared): in the order of their beginnings, against what reaches furthest so far
   std::sort(ranges.begin(), ranges.end(), [](const Range &a, const Range &b) { return a.from < b.from; });
   uintptr_t written_to = 0, read_to = 0;
   for (const Range &r : ranges) {
-    if (r.from < written_to || (r.written && r.from < read_to)) return "a buffer of tensor " + std::to_string(r.tensor) + " overlaps one that the step writes";
+    if (r.from < written_to || (r.written && r.from < read_to)) {
+      // (grad_scale may be the one that it meets)
+      if (r.tensor < 0 || (grad_scale && r.from < reinterpret_cast<uintptr_t>(grad_scale + 1) && r.to > reinterpret_cast<uintptr_t>(grad_scale))) return "grad_scale lies in a buffer that the step writes";
+      return "a buffer of tensor " + std::to_string(r.tensor) + " overlaps one that the step writes";
+    }
     (r.written ? written_to : read_to) = std::max(r.written ? written_to : read_to, r.to);
   }
   return std::string();
@@ -338,7 +347,7 @@ extern "C" int gnntrain_adamw_step(const gnntrain_adamw_tensor *tensors, int32_t
   if (n < 0 || (n > 0 && !tensors)) return train_error(GNNSTAGE_EINVAL, std::string(me) + "n must not be negative, nor tensors NULL");
   if (t < 1) return train_error(GNNSTAGE_EINVAL, std::string(me) + "t counts from 1");
   if (!(beta1 >= 0.f && beta1 < 1.f && beta2 >= 0.f && beta2 < 1.f)) return train_error(GNNSTAGE_EINVAL, std::string(me) + "beta1 and beta2 must be in [0, 1)");
-  const std::string err = adamw_check(tensors, n, state_bits);
+  const std::string err = adamw_check(tensors, n, state_bits, grad_scale);
   if (!err.empty()) return train_error(GNNSTAGE_EINVAL, me + err);
   const int e = launch_adamw(tensors, n, state_bits, AdamwRates{lr, beta1, beta2, eps}, grad_scale, t, seed, static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return train_error(GNNSTAGE_EHIP, me + std::string(hipGetErrorString((hipError_t)e)));

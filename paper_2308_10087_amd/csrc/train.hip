@@ -567,7 +567,7 @@ extern "C" int gnntrain_create(const gnntrain_desc *d, gnntrain_t **out) try {
       t.weight_decay = d->weight_decay;
       tr->adamw.push_back(t);
     }
-    err = adamw_check(tr->adamw.data(), (int)tr->adamw.size(), tr->state_bits);
+    err = adamw_check(tr->adamw.data(), (int)tr->adamw.size(), tr->state_bits, nullptr);
     if (err.empty() && !(d->beta1 >= 0.f && d->beta1 < 1.f && d->beta2 >= 0.f && d->beta2 < 1.f)) err = "beta1 and beta2 must be in [0, 1)";
     if (!err.empty()) return bad(GNNSTAGE_EINVAL, "AdamW: " + err);
   }
