@@ -10,7 +10,9 @@
 //   y = |x| / 2^e, its spacing s = 2^(max(binade of y, -6) - 3), code of s floor(y / s + u),  u of 0 .. 65535 / 65536
 //
 // The rounding is a draw, up with the probability of y's place between its neighbours: v moves by a thousandth of itself per step, codes are
-// 6 to 12 % apart, so that nearest rounding would leave it where it is for good; a draw keeps the mean.  r > 0 does not become 0 (that would
+// 6 to 12 % apart, so that nearest rounding would leave it where it is for good; a draw keeps the mean of r.  That of v = r^2 then has the draws' variance in it: a step moves r by
+// D = (1 - b2) |g^2 - v| / (2 r) off a code, of which a draw makes up to D s of variance, which decays by b2 a step: v is too large by up to E|g^2 - v| s / (2 r), whatever b2 is (less than 14 %
+// of it down to 2^-14 of the block's largest root; 3 to 4 % for normal gradients, 6 % for such of one step in fifty).  r > 0 does not become 0 (that would
 // divide by eps alone): it is rounded to the least code at least.  The draws are SplitMix64's (Steele, Lea, Flood 2014): elements 2 j and 2 j + 1
 // of a tensor have the low and the high half of the output for state key + (j + 1) gamma, 16 bits for m and 16 above them for r; tensor k's key is
 // the output for state output(seed + t gamma) + (k + 1) gamma.

@@ -1,0 +1,58 @@
+"""How far the mean of squares that 8-bit states keep is from the one of 64 bits, by the formula alone (no GPU).
+
+A draw keeps the mean of the root r, so of v = r^2 it adds its variance: a value D off a code, in a spacing s, has D (s - D) <= D s of it.  A step leaves a code by
+D = (1 - b2) |g^2 - r^2| / (2 r), and what it added decays by b2 a step: in the mean v8 - v <= E|g^2 - v8| s / (2 r), whatever b2 is.  Down to 2^-14 of the block's largest root s <= r / 8,
+and E|g^2 - v8| <= v + v8: v8 <= 17 / 15 v (and a sixtieth of
+the excess more where a step is about a spacing wide: s is then of the value that is reached).  Its variance is what was added before it decays, by 2 r to the root's: a root scatters by 0.13 - 0.17 of itself, its square by twice that; over
+2,048 elements and three spans of 1 / (1 - b2) steps a mean ratio then has a deviation of at most 0.34 / sqrt(6144) < 0.0045, of which six are allowed."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import adamw_formula as formula
+
+N, STEPS, NOISE = 2048, 6000, 6 * 0.0045
+F = np.float32
+
+
+@pytest.fixture(scope="module")
+def ratios():
+    """v8 / v, both averaged over the second half of the steps, by the gradients' kind"""
+    rng = np.random.default_rng(0)
+    few = (np.arange(N) % 32 == 0)  # a block's large elements, for those that are small beside them
+    size = {"normal": np.ones(N), "normal, near a border": np.full(N, 1.7), "one in fifty": np.ones(N)}
+    size.update({k: np.where(few, 1.0, 2.0 ** -k) for k in (13, 15, 17, 19)})
+    size = {k: x.astype(F) for k, x in size.items()}
+    n = N * len(size)
+    code, scale, v, sums = np.zeros(n, np.uint8), np.zeros(n // 32, np.uint8), np.zeros(n), np.zeros((2, n))
+    all_sizes, rare = np.concatenate(list(size.values())), np.repeat([k == "one in fifty" for k in size], N)
+    for t in range(STEPS):
+        g = rng.standard_normal(n, dtype=F) * all_sizes
+        g[rare & (rng.random(n) >= 0.02)] = 0
+        r = formula.decode(code, scale).astype(F)
+        root = formula.means_32(g, np.zeros(n), r * r, 0.9, 0.999)[1]
+        code, scale = formula.encode(root, rng.integers(0, 65536, n), True)
+        v = 0.999 * v + 0.001 * g.astype(np.float64) ** 2
+        if t >= STEPS // 2:
+            sums += formula.decode(code, scale) ** 2, v
+    parts = {k: sums[:, i * N:(i + 1) * N] for i, k in enumerate(size)}
+    return {k: float(np.divide(*(x[:, ~few] if isinstance(k, int) else x).sum(1))) for k, x in parts.items()}
+
+
+@pytest.mark.parametrize("kind", ["normal", "normal, near a border", "one in fifty", 13])
+def test_the_mean_of_squares_is_a_few_percent_too_large(ratios, kind):
+    assert 1 - NOISE <= ratios[kind] <= 17 / 15 + NOISE
+
+
+@pytest.mark.parametrize("kind,percent", [("normal", 3.4), ("normal, near a border", 3.5), ("one in fifty", 5.7), (13, 3.4)])
+def test_by_the_stated_share(ratios, kind, percent):
+    """What the header states: 3 to 4 % for normal gradients, 6 % for those of one step in fifty"""
+    assert abs(100 * (ratios[kind] - 1) - percent) <= 100 * NOISE
+
+
+@pytest.mark.parametrize("kind,low,high", [(15, 1.05, 1.25), (17, 1.4, 2.2), (19, 10, 20)])
+def test_far_below_the_largest_of_a_block(ratios, kind, low, high):
+    """The least codes are 2^-17 apart where the largest root is 1: at 2^-15 of it a quarter of the value, v8 up to E|g^2 - v8| / 8 too large, E|g^2 / v - 1| = 0.97 for normal gradients: 1.12
+    (1.25 where the largest is above 1.75, and the spacing twice that); at 2^-17 the value itself is the least code; at 2^-19 the least code, four times it, is held: 16 times v."""
+    assert low <= ratios[kind] <= high
