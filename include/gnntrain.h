@@ -60,7 +60,8 @@ typedef struct {
   int32_t n_params;
   const gnntrain_param *params; /* HOST array */
   int32_t optimizer;            /* GNNTRAIN_SGD: p -= lr (g + wd p);  GNNTRAIN_ADAM: Kingma & Ba, Algorithm 1 (wd p is added to g);
-                                   GNNTRAIN_ADAMW: gnntrain_adamw_step (wd apart from g; buffers of parameters may then not overlap) */
+                                   GNNTRAIN_ADAMW: gnntrain_adamw_step (wd apart from g, the same for every parameter: biases
+                                   and norm vectors too; buffers of parameters may then not overlap) */
   float lr, beta1, beta2, eps, weight_decay;
   int32_t shuffle;    /* 0: chunks in index order every epoch */
   uint64_t seed;      /* of the chunk shuffling, and of the dropout decisions of stages that have dropout: stage s
@@ -203,7 +204,9 @@ int gnntrain_adam_step(float *p, const float *g, float *m, float *v, void *compu
  * o(key + (j + 1) gamma), of which the low 16 bits are m's and the high ones v's.  The same call gives the same bits.
  * tensors: HOST, n of them, read during the call.  p (fp32), g (of g_dtype), compute (of compute_dtype, or NULL, or p): DEVICE, count elements, at any multiple of
  * their elements' size; m, v: DEVICE, count floats or bytes, at multiples of four bytes.  Buffers that are written may not overlap any other (gradients may
- * be shared).  count in [0, 2^35].  t = 1, 2, ...: a host number, as lr is, so that a captured call repeats its step.  grad_scale: DEVICE, one
+ * be shared).  count in [0, 2^35].  t = 1, 2, ...: a host number, as lr and seed are, so that a captured call repeats its step:
+ * the same bias correction, and with 8-bit states the same draws every time, whose mean then is not kept (an element whose draw is low never moves up: replays that train need 32 bits,
+ * or a graph per step).  grad_scale: DEVICE, one
  * float in no buffer that is written (what clips the gradients' norm, say), or NULL: 1.  beta1, beta2 in [0, 1).  Asynchronous, needs no workspace.
  * Message of an error: gnntrain_last_error(NULL). */
 typedef struct {

@@ -56,3 +56,21 @@ def test_far_below_the_largest_of_a_block(ratios, kind, low, high):
     """The least codes are 2^-17 apart where the largest root is 1: at 2^-15 of it a quarter of the value, v8 up to E|g^2 - v8| / 8 too large, E|g^2 / v - 1| = 0.97 for normal gradients: 1.12
     (1.25 where the largest is above 1.75, and the spacing twice that); at 2^-17 the value itself is the least code; at 2^-19 the least code, four times it, is held: 16 times v."""
     assert low <= ratios[kind] <= high
+
+
+def test_draws_that_repeat_keep_no_mean():
+    """A captured step that is replayed has the same draws every time.  Under a constant gradient g from a tenth of it a root moves by D = (g^2 - r^2) / (2000 r), and up by a code only where
+    D / s + u reaches 1; s is r / 16 at least, so that r stops a code past (g / r)^2 - 1 = 125 (1 - u) at the latest: below a half of g for every draw of u < 0.9."""
+    rng = np.random.default_rng(5)
+    roots = {}
+    for repeated in (True, False):
+        u = rng.integers(0, 65536, N)
+        code, scale = formula.encode(np.full(N, 0.1, F), np.full(N, 0), True)
+        for _ in range(4000):
+            r = formula.decode(code, scale).astype(F)
+            root = formula.means_32(np.ones(N, F), np.zeros(N), r * r, 0.9, 0.999)[1]
+            code, scale = formula.encode(root, u if repeated else rng.integers(0, 65536, N), True)
+        roots[repeated] = formula.decode(code, scale), u
+    stopped, u = roots[True]
+    assert np.all(stopped[u < 0.9 * 65536] < 0.5)
+    assert abs(roots[False][0].mean() - 1) < 0.05  # (from 0.1 on, e^-4 of the way in v is left)
