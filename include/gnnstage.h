@@ -409,7 +409,9 @@ int gnnstage_rows8_weight_grad(const int8_t *q, int64_t ld_q, const uint8_t *sca
  *   gnnstage_rows4_store_columns  the same from the columns of x (d x rows, ld_x >= rows): a classifier's W (d x n_classes) as one row per class
  *   gnnstage_rows4_load           x from q, scale
  *   gnnstage_rows4_product        out (rows x others) = stored rows times other stored rows, over their d columns, + bias (DEVICE fp32, others elements, or NULL): products
- *                                 of exactly the stored values, fp32 sums in a fixed order, rounded once.  others at most 2^29
+ *                                 of exactly the stored values, fp32 sums in a fixed order, rounded once: off by at most (d + 2) 2^-24 of the sum of the terms'
+ *                                 magnitudes and (d + 1) 2^-126; finite where that sum is below 2^127, otherwise possibly infinite or, with both signs, no number.
+ *                                 others at most 2^29
  * They only launch kernels on hip_stream.  Message of an error: gnnstage_last_error(NULL).
  */
 int gnnstage_rows4_store(const void *x, int32_t dtype, int64_t ld_x, int64_t rows, int32_t d, uint8_t *q, int64_t ld_q, uint8_t *scale,

@@ -44,7 +44,6 @@ def _blocks(rng, rows, d, lo, hi):
 
 
 def _product(a, b, bias, out_dtype=torch.float32):
-    """A product and its transposed one, with the other rows as the given ones, the same as the plain one's bits"""
     g = _g()
     (qa, sa, A), (qb, sb, B) = a, b
     out = torch.empty(A.shape[0], B.shape[0], dtype=out_dtype, device=DEV)
