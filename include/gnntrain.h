@@ -45,6 +45,7 @@ typedef struct {
   int64_t count;
 } gnntrain_param;
 
+/* New fields come at the end, and zero keeps what was: clear the struct before filling it in, and build callers against the header of their library (it has no size field). */
 typedef struct {
   int32_t n_stages;
   gnnstage_t *const *stages; /* HOST array, first to last; same graph size and chunks for all */
@@ -148,9 +149,10 @@ int gnntrain_head_xent(const void *h, int64_t ld_h, const void *W, int32_t dtype
  *   norm     (largest z that is a number, log sum_c exp(z_c - largest z)): what gnntrain_logprobs_grad takes, rows x 2
  *   top_ids, top_logp  the n_top classes of the largest z in their order, of equals the lower class first, and their log softmax, rows x n_top
  * Each output but the last two, which n_top > 0 asks for, may be NULL.  Sums are fp32; a row that is sure of its given class has a log probability with all its digits.
+ * Where it is sure of another class, log sum (with entropy and top_logp, which have it in them) is off by up to 2^-24 next to 1: the top_logp of a probability within that of 1 is 0.
  * A logit of minus infinity is a class left out: probability 0, last in the order.  A row whose every logit is minus infinity, or with infinity or a NaN among
  * them, has NaN for every number but norm's first; a NaN is in no order, and ids that are not there are -1.  A row whose mask byte is 0 (mask NULL: none) takes
- * no part, whatever it holds: it gets zeros, classes -1 and their log probabilities minus infinity.
+ * no part, whatever it holds (its memory may be read all the same): it gets zeros, classes -1 and their log probabilities minus infinity.
  * logits: DEVICE rows x n_classes of dtype, leading dimension ld >= n_classes, aligned to its elements; bias: DEVICE fp32 n_classes or NULL; ids, mask: DEVICE, by row, or NULL.
  * n_classes in [1, 2^24], n_top in [0, 64] and n_classes at most.  workspace: DEVICE, 256-byte aligned, of gnntrain_logprobs_workspace_size(), nothing in it
  * has to be cleared or kept; calls that overlap in time need workspaces of their own, and so do graphs that are replayed side by side.  Outputs may not
@@ -163,7 +165,7 @@ int gnntrain_logprobs(const void *logits, int32_t dtype, int64_t ld, const float
 /* Gradient of the logits from those of logp and entropy (g_logp, g_entropy: DEVICE fp32 by row; NULL: zeros):
  *   dlogits_c = g_logp ([c = id] - p_c) - g_entropy p_c (log p_c + entropy);  dbias_c += sum over the rows of dlogits_c before it is rounded
  * logits, bias, ids, mask as in the forward call, logp (with g_logp), entropy (with g_entropy) and norm what it gave.  A row without a class in [0, n_classes) has
- * no part in g_logp; a row whose mask byte is 0 gets zeros, whatever it holds.  dlogits: DEVICE rows x n_classes of dl_dtype, leading dimension ld_dl >= n_classes (columns
+ * no part in g_logp; a row whose mask byte is 0 gets zeros, whatever it holds (it may be read).  dlogits: DEVICE rows x n_classes of dl_dtype, leading dimension ld_dl >= n_classes (columns
  * behind n_classes stay as they are); it may be logits, with the same type and leading dimension.  dbias: DEVICE fp32 n_classes or NULL.  Sums in a fixed order.
  * workspace as above, of gnntrain_logprobs_grad_workspace_size(). */
 size_t gnntrain_logprobs_grad_workspace_size(int64_t rows, int32_t n_classes);

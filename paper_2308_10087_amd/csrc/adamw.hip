@@ -226,8 +226,9 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Args a) {
   }
 }
 
-// Elements from which fp32 states take four parts a workgroup, which have four times the loads in flight.  In us, one part / four: 2^26 elements, fp32 356 / 347, 8 bits 193 / 208; 18
-// tensors of 276 k elements, fp32 4.5 / 9.0.
+// Elements from which fp32 states take four parts a workgroup, which have four times the loads in flight.  The kernel in us, one part / four, with a bf16 copy: one tensor of 2^18 elements 3.2 /
+// 5.0, 2^20 5.5 / 6.7, 2^21 8.8 / 9.2, 2^22 21.0 / 19.3, 2^23 38.2 / 37.9, 2^26 369 / 371; 18 tensors of 2^18 in all 3.5 / 6.4, 2^21 9.6 / 11.0, 2^22 19.8 / 20.7, 2^23 39.3 / 38.8, 2^26 418 / 394.  8
+// bits stay with one (2^26: 193 / 208).
 constexpr int64_t kManyElements = 1 << 21;
 
 }  // namespace

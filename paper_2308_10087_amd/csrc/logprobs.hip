@@ -12,8 +12,8 @@
 // Best classes: a wave keeps the 64 best of what it has seen in its lanes, in order, as 64-bit keys (the logit's bits in the numbers' order, then the
 // class turned over, so that of equals the lower class is the larger key).  A logit has to be above a border to be looked at: one comparison per vector.  The border is what is
 // known to be below n_top others: the n_top-th of the first whole step's lanes' largest, then of the wave's list, or what another wave of the row has found.  Those that are above
-// wait in LDS until there are 16 (of more than 16 best: 64), which are sorted and merged in.  (Without the first step's border, and merged 64 at a time, 8,191 x 100,003 bf16 with
-// ten best took 26 % more vector instructions, 474 us for 417.)
+// wait in LDS until there are 16 (of more than 16 best: 64), which are sorted and merged in.  (8,191 x 100,003 bf16 with ten best: 170 M vector
+// instructions, 429 us; without the first step's border 436, merged 64 at a time 434, both 182 M and 443; without any best classes 407.)
 #include <hip/hip_runtime.h>
 #include "guard.h"
 
@@ -390,7 +390,8 @@ __device__ __forceinline__ int given_class(const AnswerArgs &a, int64_t r) {
 }
 
 // Rows of few classes, at most N LANES: LANES (2 or 4) lanes each, with their logits in registers, so that what a row costs is its classes and not the lanes'
-// meetings.  Bound by the chain of a wave's life: loads in four round trips, LDS, a search per best class (232,965 x 41 fp32, 3 best, 66 % of the rows: 18 us, the bytes alone 6).  A
+// meetings.  Bound by the chain of a wave's life: loads in four round trips, LDS, a search per best class (232,965 x 41 fp32, 3 best, 66 % of the rows: 18 us, the bytes alone 6), and by where it
+// begins: 6,400 bytes of LDS let 25 waves onto a CU, 28.4 of which are its share there.  Rows that take no part are loaded as well: 17, 18, 18, 16 us with all, 66, 30 and 2 % of them.  A
 // wave's rows go through LDS, kPitch floats apart: LANES times an odd number, in which lanes meet in no bank.
 template <typename T, int LANES, int N>
 __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
@@ -492,8 +493,8 @@ __global__ __launch_bounds__(64) void answer_short_kernel(const AnswerArgs a) {
   }
 }
 
-// A wave per row (WAVES 1: four rows per workgroup), or a workgroup of four waves per row or part of one.  Bound by the vector units next to memory: a logit takes about ten
-// instructions and an exponential (8,191 x 100,003 bf16 with bias, ten best: 400 us, 4.1 TB/s; reads alone would take 268).
+// A wave per row (WAVES 1: four rows per workgroup), or a workgroup of four waves per row or part of one.  Bound by the vector units next to memory: 64 logits take 13
+// vector instructions, one of them the exponential (8,191 x 100,003 bf16 with bias, ten best: 170 M of them, 400 us, 4.1 TB/s; reads alone would take 268).
 template <typename T, bool TOP, bool BIAS, int WAVES>
 __global__ __launch_bounds__(256) void answer_kernel(const AnswerArgs a) {
   __shared__ Key room[TOP ? 4 * kWaiting : 1];
@@ -851,7 +852,9 @@ GradPlan grad_plan(int64_t rows, int C, int n) {
   p.blocks = (C + p.across * n - 1) / (p.across * n);
   const int64_t down = 256 / p.across;
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kPartElements / C, kMostBlocks / 2 / p.blocks));
-  // Workgroups that end soon keep in step with those beside them (rows of 200 KB at odd places, copied: 32 rows each 5.2 TB/s, 195 4.5), 2,048 of them at least.
+  // Workgroups that end soon keep in step with those beside them (rows of 200 KB at odd places, copied: 32 rows each 5.2 TB/s, 195 4.5), 2,048 of them at least.  In us, with 512 / 1,024 /
+  // 2,048 / 4,096 at least, dbias among them: 232,965 x 41 fp32 34 / 25 / 28 / 27, 70,001 x 172 fp32 24.5 / 24.6 / 26.6 / 31.7, bf16 33 / 40 / 39 / 39, 20,000 x 1,000 fp32 35 / 35 / 36 / 42,
+  // 8,191 x 100,003 bf16 716 with any.
   const int64_t few = std::max<int64_t>(kAhead * down, (rows * p.blocks + 2047) / 2048);
   p.rows_per = std::max<int64_t>(std::min<int64_t>(kChain * down, few), (rows + most - 1) / most);
   p.groups = std::max<int64_t>(1, (rows + p.rows_per - 1) / p.rows_per);

@@ -170,7 +170,8 @@ __global__ __launch_bounds__(256) void rows4_store_kernel(const T *x, int64_t ld
   }
 }
 
-// The columns of x (d x rows) as rows: a thread per block, 64 columns and four blocks down a workgroup.
+// The columns of x (d x rows) as rows: a thread per block, 64 columns and four blocks down a workgroup.  256 x 100,003 fp32 25 us (4.7 TB/s), bf16 29 us (2.3 TB/s: an instruction's loads are 128
+// bytes of a row); 256 x 400,009 106 and 97 us.
 template <typename T>
 __global__ __launch_bounds__(256) void rows4_store_columns_kernel(const T *x, int64_t ld, int64_t rows, int d, int blocks, uint8_t *q, int64_t ld_q, uint8_t *scale,
                                                                   int64_t ld_s) {
@@ -290,7 +291,8 @@ __device__ __forceinline__ f32x16 multiply(const Operand &a, const Operand &b, f
 // A wave owns 32 kAcross columns and goes down `per` tiles of 32 rows.  A lane's columns are side by side (column kAcross l + t is the t-th instruction's l-th), so that
 // rows are written 256 (fp32: 512) bytes at a time from the registers.  Register i of lane l: row 8 (i / 4) + 4 (l / 32) + i % 4.
 // Bound by the results' writes: 8,191 x 100,003 x 256 to bf16 365 us, 4.5 TB/s (rows of 200,006 bytes: two workgroups share a line; at whole lines 5.4 - 5.9), matrix cores 0.2 of
-// the time; 3 x 400,009 x 256 by the other operands, 54 MB in 15 us.
+// the time; 3 x 400,009 x 256 by the other operands, 54 MB in 15.5 us: 784 workgroups, 512 of which are there at a time.  Beyond 256 columns operands are loaded for every tile when it needs
+// them: 8,191 x 100,003 x 512 1,340 us, x 602 1,640.
 // ONE: up to 256 columns of operands, those of the wave's columns stay in registers and the next rows' are on their way.
 constexpr int kAcross = 4;
 constexpr int kGroup = 4;  // waves of a workgroup (2 / 4 / 8: 441 / 371 / 399 - 476 us)
